@@ -329,6 +329,119 @@ rp_status rp_decode_step_static(const rp_model *model, void *stream, int32_t B, 
                                 int32_t *next_ids);
 
 /* ---------------------------------------------------------------------------
+ * Rollout cache in pages (Section "Prefix Sharing": the N sampled responses of
+ * a GRPO prompt group share one prefix; a rollout's sequences grow and end at
+ * different times).  A pool of n_pages pages of page_size tokens holds the keys
+ * and values of every layer; sequence b's token t lies in page
+ * table[b*table_ld + t/page_size], slot t % page_size.  All members are the
+ * caller's device memory, read and written by the calls below in stream order:
+ *   kv      the pool: row p*page_size + s of a layer is slot s of page p, rows of
+ *           [n_kv_heads][head_dim] (16-byte multiples), layer l at l*layer_stride
+ *           elements (layer_stride >= n_pages*page_size rows).  K after RoPE.
+ *   table   int32 [n_seqs][table_ld]; entries past a sequence's pages are not read
+ *   len     int32 [n_seqs]: tokens held; ceil(len/page_size) entries are in use
+ *   refs    int32 [n_pages]: table entries in use that hold the page, 0 = free
+ * page_size is a power of two in [8, 1024] and table_ld*page_size < 2^31.  An
+ * empty pool is len = 0 and refs = 0.  A full page may be shared; the page that a
+ * sequence writes next never is.  The calls enqueue kernels only (no allocation,
+ * copy or synchronisation), so they can be captured in a HIP graph.  Calls that
+ * change one pool are ordered by the caller (one stream, or events).  Lengths
+ * outside [0, table_ld*page_size] are clamped and page ids outside [0, n_pages)
+ * are skipped (attention: clamped), so bad device values never reach memory
+ * outside the pool.  Host lists (seqs, src, dst: int32 [n], n in [1,
+ * RP_MAX_SEQS]) hold indices in [0, n_seqs), each once where it is written, else
+ * RP_ERR_SHAPE.
+ *
+ * Pages are taken lowest free id first, in list order.  A sequence that needs new
+ * pages gets them if the needs of the list up to and with its own are no more
+ * than the free pages; otherwise it stays as it was and missing[i] (dev int32,
+ * required) says how many of its pages there were not, or -1 where its tokens
+ * exceed table_ld pages.  missing[i] = 0: done.
+ *
+ * rp_pages_append  row r of rows (packed [R][n_kv_heads][head_dim] per layer, as
+ *   rp_prefix_forward leaves kv_out; layer_stride elements apart), cu[i] <= r <
+ *   cu[i+1], becomes the next token of sequence seqs[i] (cu: host int32 [n+1],
+ *   cu[0] = 0, non-decreasing; rows may be NULL where cu[n] = 0).
+ * rp_pages_fork    sequence dst[i] gives its pages back and becomes a copy of
+ *   src[i]: full pages are shared, the rows of a last, partial one are copied to a
+ *   page of its own.  All dst are freed before the first page is taken; a dst that
+ *   gets no page stays empty.  src may repeat; no dst may be a src.
+ * rp_pages_free    sequences seqs[i] give their pages back (len 0, entries -1).
+ * rp_pages_compact pages in use with ids >= n_live (their number) move to the free
+ *   ids below it, both in ascending order: contents, tables and refs.  n_live
+ *   (optional dev int32 [1]) receives the number.  workspace >=
+ *   rp_pages_compact_workspace_bytes().
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  rp_kv kv;
+  rp_dtype dtype;
+  int32_t n_layers, n_kv_heads, head_dim;
+  int32_t n_pages, page_size;
+  int32_t *table, *len, *refs;
+  int32_t n_seqs, table_ld;
+} rp_pages;
+
+rp_status rp_pages_append(const rp_pages *pages, void *stream, int32_t n, const int32_t *seqs_host,
+                          const int32_t *cu_host, rp_kv rows, int32_t *missing);
+rp_status rp_pages_fork(const rp_pages *pages, void *stream, int32_t n, const int32_t *src_host,
+                        const int32_t *dst_host, int32_t *missing);
+rp_status rp_pages_free(const rp_pages *pages, void *stream, int32_t n, const int32_t *seqs_host);
+rp_status rp_pages_compact_workspace_bytes(const rp_pages *pages, size_t *bytes);
+rp_status rp_pages_compact(const rp_pages *pages, void *stream, int32_t *n_live, void *workspace,
+                           size_t workspace_bytes);
+
+/* ---------------------------------------------------------------------------
+ * Drafted trees over the paged cache (the rollout side of Eq. (1): a decode step
+ * is bound by the cache it reads, so a step that checks several drafted tokens a
+ * sequence costs little more than one).  Batch entry b is table row b, b < B <=
+ * n_seqs; it has n_nodes[b] new tokens (dev int32 [B], clamped to [0, N]; NULL =
+ * N) in rows b*N .. of arrays of B*N rows, N in [1, RP_MAX_NODES]; rows past
+ * n_nodes[b] are padding.
+ *
+ * rp_tree_attention  grouped-query attention of the new tokens of one layer: row i
+ *   of b attends to the len[b] cached tokens and to the new tokens j < n_nodes[b]
+ *   whose bit j%32 of mask[(b*N+i)*ceil(N/32) + j/32] (dev uint32) is set; mask
+ *   NULL: to the new tokens j <= i (one new token: N = 1).  out row = sum_j
+ *   softmax_j(scale q.k_j) v_j; a row that sees nothing is 0.  Values of tokens
+ *   that a row does not see do not enter it, whatever they are.  q: rows q_ld
+ *   elements apart (q_ld >= n_q_heads*head_dim, a multiple of 8), head h at column
+ *   h*head_dim; k_new, v_new: [B*N][n_kv_heads][head_dim]; out [B*N][n_q_heads*
+ *   head_dim], padding rows are left as they were.  head_dim 64 or 128, at most 8 q
+ *   heads per kv head.  The order of the sums depends on the batch.
+ * rp_tree_step  one forward pass of the model over the new tokens: token_ids [B*N]
+ *   (dev int32), trees by parents (dev int32 [B*N], the index of a node's parent
+ *   among its sequence's; outside [0, i) = none; NULL = chains i-1), node i at rotary position
+ *   pos0[b] + its depth (pos0 dev int32 [B]; NULL = len[b], after M-RoPE prompts
+ *   the next rotary position).  A node sees the cache, its ancestors and itself.
+ *   draft receives the new tokens' K/V of every layer ([B*N] rows, layer_stride
+ *   apart), logits (optional fp32 [B*N, V]) their logits and next_ids [B*N] the
+ *   argmax (lowest id on ties); padding rows hold unspecified numbers.  The cache is read only.
+ *   The pool's type, layers and heads are the model's.  bf16 models at
+ *   head_dim 64 return RP_ERR_UNSUPPORTED, as rp_decode_step does.
+ * rp_tree_commit  the path that the model's choices next_ids (dev int32 [B*N],
+ *   argmax or samples) confirm: from node 0, the next node is the first child whose token is
+ *   next_ids of the present one.  accepted [B*N] receives the path's nodes (then -1),
+ *   n_accepted [B] their number, token_out [B] the choice after the last of them (-1 for a
+ *   sequence without nodes); their K/V rows are appended to sequence b as by rp_pages_append
+ *   (a sequence without room: n_accepted 0, token_out -1).  B <= 4096.
+ * ------------------------------------------------------------------------- */
+#define RP_MAX_NODES 256 /* new tokens of a sequence */
+rp_status rp_tree_attention_workspace_bytes(const rp_pages *pages, int32_t B, int32_t N, int32_t n_q_heads,
+                                            size_t *bytes);
+rp_status rp_tree_attention(const rp_pages *pages, void *stream, int32_t layer, int32_t B, int32_t N,
+                            int32_t n_q_heads, const int32_t *n_nodes, const uint32_t *mask, const void *q,
+                            int64_t q_ld, const void *k_new, const void *v_new, float scale, void *out,
+                            void *workspace, size_t workspace_bytes);
+rp_status rp_tree_step_workspace_bytes(const rp_model *model, int32_t B, int32_t N, size_t *bytes);
+rp_status rp_tree_step(const rp_model *model, void *stream, const rp_pages *pages, int32_t B, int32_t N,
+                       const int32_t *n_nodes, const int32_t *token_ids, const int32_t *parents,
+                       const int32_t *pos0, rp_kv draft, float *logits, int32_t *next_ids, void *workspace,
+                       size_t workspace_bytes);
+rp_status rp_tree_commit(const rp_pages *pages, void *stream, int32_t B, int32_t N, const int32_t *n_nodes,
+                         const int32_t *token_ids, const int32_t *parents, const int32_t *next_ids, rp_kv draft,
+                         int32_t *accepted, int32_t *n_accepted, int32_t *token_out, int32_t *missing);
+
+/* ---------------------------------------------------------------------------
  * Co-location helpers (Section "Resource Sharing Policy": decode and prefix
  * share one GPU; static partitions are the analog of the paper's SM
  * partitions).  mask: n_words 32-bit words, bit i = compute unit i may run

@@ -26,12 +26,16 @@ RP_MAX_SEQS = 256
 RP_SUFFIX_FUSED_LOGPROB = 1
 RP_WO_TRANSPOSED, RP_W_DOWN_TRANSPOSED = 1, 2
 RP_PREFIX_LAST_ROWS_ONLY = 1
+RP_MAX_NODES = 256
 SYMBOLS = ["rp_create", "rp_destroy", "rp_prefix_workspace_bytes", "rp_prefix_forward", "rp_prefix_forward_mrope",
            "rp_prefix_forward_flags",
            "rp_suffix_workspace_bytes", "rp_suffix_logprob", "rp_suffix_grouped_workspace_bytes",
            "rp_suffix_logprob_grouped", "rp_prompt_logprob_workspace_bytes", "rp_prompt_logprob",
            "rp_decode_workspace_bytes",
-           "rp_decode_step", "rp_decode_step_static", "rp_stream_create_cu_masked", "rp_stream_destroy",
+           "rp_decode_step", "rp_decode_step_static",
+           "rp_pages_append", "rp_pages_fork", "rp_pages_free", "rp_pages_compact_workspace_bytes", "rp_pages_compact",
+           "rp_tree_attention_workspace_bytes", "rp_tree_attention", "rp_tree_step_workspace_bytes", "rp_tree_step",
+           "rp_tree_commit", "rp_stream_create_cu_masked", "rp_stream_destroy",
            "rp_device_cu_count", "rp_calibrate_mfma", "rp_calibrate_read", "rp_last_error", "rp_status_string", "rp_version",
            "rp_profile_enable", "rp_profile_collect", "rp_profile_count", "rp_profile_read",
            "rp_profile_reset"]
@@ -62,6 +66,12 @@ class RpWeights(Structure):
 
 class RpKV(Structure):
     _fields_ = [("k", c_void_p), ("v", c_void_p), ("layer_stride", c_int64)]
+
+
+class RpPages(Structure):
+    _fields_ = [("kv", RpKV), ("dtype", c_int), ("n_layers", c_int32), ("n_kv_heads", c_int32), ("head_dim", c_int32),
+                ("n_pages", c_int32), ("page_size", c_int32), ("table", c_void_p), ("len", c_void_p), ("refs", c_void_p),
+                ("n_seqs", c_int32), ("table_ld", c_int32)]
 
 
 _lib = None
@@ -107,6 +117,20 @@ def lib():
                                        c_void_p, c_void_p, c_void_p, c_size_t]),
             "rp_decode_step_static": (c_int, [c_void_p, c_void_p, c_int32, RpKV, c_int32, c_void_p, c_void_p,
                                               c_void_p, c_void_p]),
+            "rp_pages_append": (c_int, [POINTER(RpPages), c_void_p, c_int32, POINTER(c_int32), POINTER(c_int32), RpKV,
+                                        c_void_p]),
+            "rp_pages_fork": (c_int, [POINTER(RpPages), c_void_p, c_int32, POINTER(c_int32), POINTER(c_int32), c_void_p]),
+            "rp_pages_free": (c_int, [POINTER(RpPages), c_void_p, c_int32, POINTER(c_int32)]),
+            "rp_pages_compact_workspace_bytes": (c_int, [POINTER(RpPages), POINTER(c_size_t)]),
+            "rp_pages_compact": (c_int, [POINTER(RpPages), c_void_p, c_void_p, c_void_p, c_size_t]),
+            "rp_tree_attention_workspace_bytes": (c_int, [POINTER(RpPages), c_int32, c_int32, c_int32, POINTER(c_size_t)]),
+            "rp_tree_attention": (c_int, [POINTER(RpPages), c_void_p, c_int32, c_int32, c_int32, c_int32, c_void_p, c_void_p,
+                                          c_void_p, c_int64, c_void_p, c_void_p, c_float, c_void_p, c_void_p, c_size_t]),
+            "rp_tree_step_workspace_bytes": (c_int, [c_void_p, c_int32, c_int32, POINTER(c_size_t)]),
+            "rp_tree_step": (c_int, [c_void_p, c_void_p, POINTER(RpPages), c_int32, c_int32, c_void_p, c_void_p, c_void_p,
+                                     c_void_p, RpKV, c_void_p, c_void_p, c_void_p, c_size_t]),
+            "rp_tree_commit": (c_int, [POINTER(RpPages), c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p,
+                                       RpKV, c_void_p, c_void_p, c_void_p, c_void_p]),
             "rp_stream_create_cu_masked": (c_int, [c_int, POINTER(c_uint32), c_uint32, POINTER(c_void_p)]),
             "rp_stream_destroy": (c_int, [c_void_p]),
             "rp_device_cu_count": (c_int, [c_int]),
@@ -271,6 +295,67 @@ def rp_decode_step_static(model: int, stream, B: int, cache: RpKV, cap: int, kv_
     """rp_decode_step with the library's static scratch instead of a workspace."""
     _check(lib().rp_decode_step_static(model, _ptr(stream), B, cache, cap, _ptr(kv_len), _ptr(token_ids),
                                        _ptr(logits), _ptr(next_ids)))
+
+
+def make_pages(k, v, layer_stride: int, dtype: str, n_layers: int, n_kv_heads: int, head_dim: int, n_pages: int,
+               page_size: int, table, length, refs, n_seqs: int, table_ld: int) -> RpPages:
+    return RpPages(make_kv(k, v, layer_stride), _DTYPES[dtype], int(n_layers), int(n_kv_heads), int(head_dim),
+                   int(n_pages), int(page_size), _ptr(table), _ptr(length), _ptr(refs), int(n_seqs), int(table_ld))
+
+
+def rp_pages_append(pages: RpPages, stream, n: int, seqs, cu, rows: RpKV, missing) -> None:
+    _check(lib().rp_pages_append(byref(pages), _ptr(stream), int(n), _i32(seqs), _i32(cu), rows, _ptr(missing)))
+
+
+def rp_pages_fork(pages: RpPages, stream, n: int, src, dst, missing) -> None:
+    _check(lib().rp_pages_fork(byref(pages), _ptr(stream), int(n), _i32(src), _i32(dst), _ptr(missing)))
+
+
+def rp_pages_free(pages: RpPages, stream, n: int, seqs) -> None:
+    _check(lib().rp_pages_free(byref(pages), _ptr(stream), int(n), _i32(seqs)))
+
+
+def rp_pages_compact_workspace_bytes(pages: RpPages) -> int:
+    n = c_size_t()
+    _check(lib().rp_pages_compact_workspace_bytes(byref(pages), byref(n)))
+    return n.value
+
+
+def rp_pages_compact(pages: RpPages, stream, n_live, workspace, workspace_bytes: int) -> None:
+    _check(lib().rp_pages_compact(byref(pages), _ptr(stream), _ptr(n_live), _ptr(workspace), int(workspace_bytes)))
+
+
+def rp_tree_attention_workspace_bytes(pages: RpPages, B: int, N: int, n_q_heads: int) -> int:
+    n = c_size_t()
+    _check(lib().rp_tree_attention_workspace_bytes(byref(pages), int(B), int(N), int(n_q_heads), byref(n)))
+    return n.value
+
+
+def rp_tree_attention(pages: RpPages, stream, layer: int, B: int, N: int, n_q_heads: int, n_nodes, mask, q, q_ld: int,
+                      k_new, v_new, scale: float, out, workspace, workspace_bytes: int) -> None:
+    _check(lib().rp_tree_attention(byref(pages), _ptr(stream), int(layer), int(B), int(N), int(n_q_heads), _ptr(n_nodes),
+                                   _ptr(mask), _ptr(q), int(q_ld), _ptr(k_new), _ptr(v_new), float(scale), _ptr(out),
+                                   _ptr(workspace), int(workspace_bytes)))
+
+
+def rp_tree_step_workspace_bytes(model: int, B: int, N: int) -> int:
+    n = c_size_t()
+    _check(lib().rp_tree_step_workspace_bytes(model, int(B), int(N), byref(n)))
+    return n.value
+
+
+def rp_tree_step(model: int, stream, pages: RpPages, B: int, N: int, n_nodes, token_ids, parents, pos0, draft: RpKV,
+                 logits, next_ids, workspace, workspace_bytes: int) -> None:
+    _check(lib().rp_tree_step(model, _ptr(stream), byref(pages), int(B), int(N), _ptr(n_nodes), _ptr(token_ids),
+                              _ptr(parents), _ptr(pos0), draft, _ptr(logits), _ptr(next_ids), _ptr(workspace),
+                              int(workspace_bytes)))
+
+
+def rp_tree_commit(pages: RpPages, stream, B: int, N: int, n_nodes, token_ids, parents, next_ids, draft: RpKV,
+                   accepted, n_accepted, token_out, missing) -> None:
+    _check(lib().rp_tree_commit(byref(pages), _ptr(stream), int(B), int(N), _ptr(n_nodes), _ptr(token_ids),
+                                _ptr(parents), _ptr(next_ids), draft, _ptr(accepted), _ptr(n_accepted),
+                                _ptr(token_out), _ptr(missing)))
 
 
 def rp_stream_create_cu_masked(device: int, mask_words: Sequence[int]) -> int:

@@ -24,7 +24,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIBDIR = os.path.join(PKG, "lib")
 LIB = os.path.join(LIBDIR, "librollplex.so")
-SOURCES = ["api.cpp", "elementwise.hip", "gemm.hip", "gemm_flex.hip", "attention.hip", "calibrate.hip"]
+SOURCES = ["api.cpp", "elementwise.hip", "gemm.hip", "gemm_flex.hip", "attention.hip", "calibrate.hip",
+           "pages.hip", "tree_attention.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",

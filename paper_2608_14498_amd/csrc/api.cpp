@@ -585,6 +585,8 @@ const LayerNames kPrefixNames = {"prefix.rmsnorm", "prefix.gemm_qkv", "prefix.ro
 const LayerNames kSuffixNames = {"suffix.rmsnorm", "suffix.gemm_qkv", "suffix.rope_kv", "suffix.attention",
                                  "suffix.gemm_o_proj", "suffix.rmsnorm", "suffix.gemm_gate_up", "suffix.swiglu",
                                  "suffix.gemm_down"};
+const LayerNames kTreeNames = {"tree.rmsnorm", "tree.gemm_qkv", "tree.rope_kv", "tree.attention", "tree.gemm_o_proj",
+                               "tree.rmsnorm", "tree.gemm_gate_up", "tree.swiglu", "tree.gemm_down"};
 
 // B operands of the row-parallel projections in their stored layout (weight_layout).
 rp::BSeg wo_operand(const rp_config& c, const rp_layer_weights& lw) {
@@ -599,7 +601,7 @@ rp_status run_layer(const rp_model* m, hipStream_t s, const rp_layer_weights& lw
                     const LayerPlan& plan, float* gemm_part, const LayerNames& nm,
                     const rp::MRope& mr = rp::MRope{nullptr, 0, 0}, bool norm1_done = false,
                     const void* next_norm = nullptr, bool* next_normed = nullptr,
-                    const float2* rope_cs = nullptr) {
+                    const float2* rope_cs = nullptr, const rp::TreeArgs* tree = nullptr) {
   const rp_config& c = m->cfg;
   const rp_dtype dt = c.dtype;
   const int d = c.d_model, Hq = c.n_q_heads, Hkv = c.n_kv_heads, D = c.head_dim, F = c.ffn_dim;
@@ -633,23 +635,34 @@ rp_status run_layer(const rp_model* m, hipStream_t s, const rp_layer_weights& lw
     RP_TRY_LAUNCH_N(nm.rope, rp::launch_rope_kv(s, dt, st, w.QKV, M, Hq, Hkv, D, lw.bq, lw.bk, lw.bv, m->rope,
                                                 c.max_position, w.Q, k_out, v_out, mr));
   }
-  rp::AttnArgs a;
-  a.q = w.Q;
-  a.q_ld = hq;
-  a.k0 = k0;
-  a.v0 = v0;
-  a.k1 = k_out;
-  a.v1 = v_out;
-  a.o = w.O;
-  a.Hq = Hq;
-  a.Hkv = Hkv;
-  a.D = D;
-  a.scale = (float)(1.0 / sqrt((double)D));
-  a.long_keys = gemm_part != nullptr;  // the suffix pass
-  a.most_chunks = plan.attn_chunks;
-  a.part = gemm_part;  // (free between the q/k/v and the o projection)
-  a.part_floats = (int64_t)plan.part_floats;
-  RP_TRY_LAUNCH_N(nm.attn, rp::launch_attention(s, dt, st, a, M));
+  if (tree) {  // the rows of drafted trees over a paged cache
+    rp::TreeArgs t = *tree;
+    t.q = w.Q;
+    t.k = k0;
+    t.v = v0;
+    t.kn = k_out;
+    t.vn = v_out;
+    t.out = w.O;
+    RP_TRY_LAUNCH_N(nm.attn, rp::launch_tree_attention(s, dt, t));
+  } else {
+    rp::AttnArgs a;
+    a.q = w.Q;
+    a.q_ld = hq;
+    a.k0 = k0;
+    a.v0 = v0;
+    a.k1 = k_out;
+    a.v1 = v_out;
+    a.o = w.O;
+    a.Hq = Hq;
+    a.Hkv = Hkv;
+    a.D = D;
+    a.scale = (float)(1.0 / sqrt((double)D));
+    a.long_keys = gemm_part != nullptr;  // the suffix pass
+    a.most_chunks = plan.attn_chunks;
+    a.part = gemm_part;  // (free between the q/k/v and the o projection)
+    a.part_floats = (int64_t)plan.part_floats;
+    RP_TRY_LAUNCH_N(nm.attn, rp::launch_attention(s, dt, st, a, M));
+  }
   const rp::BSeg bo = wo_operand(c, lw);
   if (s_o > 1) {
     RP_TRY_LAUNCH_N(nm.oproj, rp::launch_gemm(s, dt, M, d, hq, w.O, hq, bo, bo.trans ? d : hq, nullptr, d,
@@ -1223,6 +1236,361 @@ rp_status rp_decode_step_static(const rp_model* m, void* stream, int32_t B, rp_k
   void* ws = nullptr;
   if ((st = static_scratch(&ws)) != RP_OK) return st;
   return decode_run(m, stream, B, cache, cap, kv_len, token_ids, logits, next_ids, ws, own_logits);
+}
+
+// ---- rollout cache in pages, drafted trees ----
+}  // extern "C"
+
+namespace {
+
+rp_status check_pages(const rp_pages* p) {
+  if (!p) return fail(RP_ERR_INVALID_ARG, "pages is NULL");
+  int dt = 0;  // (see check_config)
+  memcpy(&dt, &p->dtype, sizeof dt);
+  if (dt != RP_F32 && dt != RP_BF16 && dt != RP_F16) return fail(RP_ERR_INVALID_ARG, "pages: bad dtype %d", dt);
+  if (!p->kv.k || !p->kv.v || !p->table || !p->len || !p->refs)
+    return fail(RP_ERR_INVALID_ARG, "pages: k, v, table, len and refs are required");
+  if (!aligned16(p->kv.k) || !aligned16(p->kv.v) || p->kv.layer_stride % 8)
+    return fail(RP_ERR_INVALID_ARG, "pages: KV must be 16-byte aligned (layer_stride multiple of 8)");
+  if (p->n_layers < 1 || p->n_kv_heads < 1 || p->head_dim < 1 || p->n_pages < 1 || p->n_seqs < 1 || p->table_ld < 1)
+    return fail(RP_ERR_SHAPE, "pages: sizes must be positive");
+  if (p->page_size < 8 || p->page_size > 1024 || (p->page_size & (p->page_size - 1)))
+    return fail(RP_ERR_SHAPE, "pages: page_size %d is not a power of two in [8, 1024]", p->page_size);
+  const int64_t row = (int64_t)p->n_kv_heads * p->head_dim, es = dt == RP_F32 ? 4 : 2;
+  if (row > (1 << 20) || row * es % 16) return fail(RP_ERR_UNSUPPORTED, "pages: rows must be 16-byte multiples of at most 2^20 elements");
+  if ((int64_t)p->table_ld * p->page_size >= (int64_t)1 << 31)
+    return fail(RP_ERR_UNSUPPORTED, "pages: table_ld * page_size must be below 2^31");
+  if (p->n_layers > 32767 || (int64_t)p->n_pages * p->page_size >= (int64_t)1 << 31)
+    return fail(RP_ERR_UNSUPPORTED, "pages: too many layers or tokens");
+  if (p->kv.layer_stride < (int64_t)p->n_pages * p->page_size * row)
+    return fail(RP_ERR_SHAPE, "pages: layer_stride %lld < %lld elements", (long long)p->kv.layer_stride,
+                (long long)((int64_t)p->n_pages * p->page_size * row));
+  return RP_OK;
+}
+
+int64_t pages_elem(const rp_pages& p) { return p.dtype == RP_F32 ? 4 : 2; }
+int page_shift(const rp_pages& p) { return __builtin_ctz((unsigned)p.page_size); }
+
+rp::PageArgs page_args(const rp_pages& p) {
+  rp::PageArgs a;
+  a.k = (uint8_t*)p.kv.k;
+  a.v = (uint8_t*)p.kv.v;
+  a.layer_bytes = p.kv.layer_stride * pages_elem(p);
+  a.row_bytes = (int32_t)((int64_t)p.n_kv_heads * p.head_dim * pages_elem(p));
+  a.n_layers = p.n_layers;
+  a.n_pages = p.n_pages;
+  a.lg = page_shift(p);
+  a.table = p.table;
+  a.len = p.len;
+  a.refs = p.refs;
+  a.n_seqs = p.n_seqs;
+  a.table_ld = p.table_ld;
+  return a;
+}
+
+// A host list of sequences; distinct: each at most once.
+rp_status check_seqs(const rp_pages& p, int32_t n, const int32_t* seqs, const char* what, bool distinct) {
+  if (n < 1 || n > RP_MAX_SEQS) return fail(RP_ERR_SHAPE, "%s: count %d outside [1, %d]", what, n, RP_MAX_SEQS);
+  if (!seqs) return fail(RP_ERR_INVALID_ARG, "%s is NULL", what);
+  for (int i = 0; i < n; ++i) {
+    if (seqs[i] < 0 || seqs[i] >= p.n_seqs)
+      return fail(RP_ERR_SHAPE, "%s[%d] = %d outside [0, %d)", what, i, seqs[i], p.n_seqs);
+    for (int j = 0; distinct && j < i; ++j)
+      if (seqs[j] == seqs[i]) return fail(RP_ERR_SHAPE, "%s[%d] = %d is listed twice", what, i, seqs[i]);
+  }
+  return RP_OK;
+}
+
+// Rows handed to the pool: R rows a layer.
+rp_status check_rows(const rp_pages& p, const rp_kv& kv, int64_t R, const char* what) {
+  if (R == 0) return RP_OK;  // nothing is read
+  if (!kv.k || !kv.v) return fail(RP_ERR_INVALID_ARG, "%s: k or v is NULL", what);
+  const int64_t per = R * p.n_kv_heads * p.head_dim;
+  if (kv.layer_stride < per)
+    return fail(RP_ERR_SHAPE, "%s: layer_stride %lld < %lld elements", what, (long long)kv.layer_stride, (long long)per);
+  if (!aligned16(kv.k) || !aligned16(kv.v) || kv.layer_stride % 8)
+    return fail(RP_ERR_INVALID_ARG, "%s: KV must be 16-byte aligned (layer_stride multiple of 8)", what);
+  return RP_OK;
+}
+
+rp_status check_tree(const rp_pages& p, int32_t B, int32_t N) {
+  if (B < 1 || B > p.n_seqs) return fail(RP_ERR_SHAPE, "batch %d outside [1, n_seqs %d]", B, p.n_seqs);
+  if (N < 1 || N > RP_MAX_NODES) return fail(RP_ERR_SHAPE, "new tokens per sequence %d outside [1, %d]", N, RP_MAX_NODES);
+  if ((int64_t)B * N > 1 << 24) return fail(RP_ERR_UNSUPPORTED, "batch * new tokens exceeds 2^24");
+  return RP_OK;
+}
+
+rp_status check_tree_heads(const rp_pages& p, int32_t Hq) {
+  if (p.head_dim != 64 && p.head_dim != 128) return fail(RP_ERR_UNSUPPORTED, "head_dim %d (supported: 64, 128)", p.head_dim);
+  if (Hq < 1 || Hq % p.n_kv_heads) return fail(RP_ERR_SHAPE, "n_q_heads %d not a multiple of n_kv_heads %d", Hq, p.n_kv_heads);
+  if (Hq / p.n_kv_heads > 8) return fail(RP_ERR_UNSUPPORTED, "query group size %d > 8", Hq / p.n_kv_heads);
+  return RP_OK;
+}
+
+rp::TreeArgs tree_args(const rp_pages& p, int32_t B, int32_t N, int32_t Hq, const int32_t* n_nodes, const uint32_t* mask) {
+  rp::TreeArgs a;
+  memset(&a, 0, sizeof a);
+  a.table = p.table;
+  a.len = p.len;
+  a.n_nodes = n_nodes;
+  a.mask = mask;
+  a.n_pages = p.n_pages;
+  a.lg = page_shift(p);
+  a.table_ld = p.table_ld;
+  a.B = B;
+  a.N = N;
+  a.W = (N + 31) / 32;
+  a.Hq = Hq;
+  a.Hkv = p.n_kv_heads;
+  a.D = p.head_dim;
+  return a;
+}
+
+size_t tree_attn_ws(rp_dtype dt, int32_t B, int32_t N, int32_t Hq, int32_t Hkv, int32_t D, void* base, float** part) {
+  Carver c(base);
+  float* p = (float*)c.take(rp::tree_partial_floats(dt, B, N, Hq, Hkv, D) * 4);
+  if (part) *part = p;
+  return c.off + 256;
+}
+
+struct TreeWS {
+  LayerWS L;
+  uint32_t* mask;
+  int32_t* positions;  // [3][R]
+  float* logits;       // where the caller passes none and the argmax is not fused
+  rp::ArgmaxPart* arg_part;
+  float* attn_part;
+  float* gemm_part;
+  LayerPlan plan;
+};
+
+// Up to 64 rows run the projections as a decode step does (split to fill the chip), more as a
+// suffix pass (a row's sums do not depend on the others).
+size_t tree_ws(const rp_model* m, int32_t B, int32_t N, void* base, TreeWS* w) {
+  Carver c(base);
+  TreeWS tmp;
+  TreeWS* t = w ? w : &tmp;
+  const rp_config& cfg = m->cfg;
+  const int64_t R = (int64_t)B * N;
+  t->plan = plan_layer(cfg, (int32_t)R, R <= 64 ? Pass::kDecode : Pass::kSuffix);
+  carve_layer(c, cfg, R, true, !t->plan.fused, &t->L);
+  t->mask = (uint32_t*)c.take(R * ((N + 31) / 32) * 4);
+  t->positions = (int32_t*)c.take(3 * R * 4);
+  const bool fused = R <= 64 && decode_fused_argmax(m, (int32_t)R);
+  t->arg_part = fused ? (rp::ArgmaxPart*)c.take(rp::gemm_argmax_parts((int32_t)R, cfg.vocab) * sizeof(rp::ArgmaxPart)) : nullptr;
+  t->logits = fused ? nullptr : (float*)c.take(R * cfg.vocab * 4);
+  t->attn_part = (float*)c.take(rp::tree_partial_floats(cfg.dtype, B, N, cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim) * 4);
+  t->gemm_part = (float*)c.take(t->plan.part_floats * 4);
+  return c.off + 256;
+}
+
+}  // namespace
+
+extern "C" {
+
+rp_status rp_pages_append(const rp_pages* pages, void* stream, int32_t n, const int32_t* seqs, const int32_t* cu, rp_kv rows,
+                          int32_t* missing) {
+  rp_status st = check_pages(pages);
+  if (st != RP_OK || (st = check_seqs(*pages, n, seqs, "seqs", true)) != RP_OK) return st;
+  if (!cu || !missing) return fail(RP_ERR_INVALID_ARG, "cu and missing are required");
+  if (cu[0] != 0) return fail(RP_ERR_SHAPE, "cu[0] = %d, must be 0", cu[0]);
+  for (int i = 0; i < n; ++i)
+    if (cu[i + 1] < cu[i]) return fail(RP_ERR_SHAPE, "cu[%d] = %d < cu[%d] = %d", i + 1, cu[i + 1], i, cu[i]);
+  if ((st = check_rows(*pages, rows, cu[n], "rows")) != RP_OK) return st;
+  hipStream_t s = (hipStream_t)stream;
+  const rp::PageArgs a = page_args(*pages);
+  rp::SeqRows q;
+  memset(&q, 0, sizeof q);
+  q.n = n;
+  for (int i = 0; i < n; ++i) q.seq[i] = seqs[i];
+  for (int i = 0; i <= n; ++i) q.cu[i] = cu[i];
+  RP_TRY_LAUNCH_N("pages.append_plan", rp::launch_append_plan(s, a, q, missing));
+  if (cu[n] > 0)
+    RP_TRY_LAUNCH_N("pages.append_rows", rp::launch_append_rows(s, a, q, rows.k, rows.v, rows.layer_stride * pages_elem(*pages),
+                                                                missing));
+  return RP_OK;
+}
+
+rp_status rp_pages_fork(const rp_pages* pages, void* stream, int32_t n, const int32_t* src, const int32_t* dst, int32_t* missing) {
+  rp_status st = check_pages(pages);
+  if (st != RP_OK || (st = check_seqs(*pages, n, src, "src", false)) != RP_OK ||
+      (st = check_seqs(*pages, n, dst, "dst", true)) != RP_OK)
+    return st;
+  if (!missing) return fail(RP_ERR_INVALID_ARG, "missing is required");
+  for (int i = 0; i < n; ++i)
+    for (int j = 0; j < n; ++j)
+      if (src[i] == dst[j]) return fail(RP_ERR_SHAPE, "sequence %d is both a src and a dst", src[i]);
+  hipStream_t s = (hipStream_t)stream;
+  const rp::PageArgs a = page_args(*pages);
+  rp::SeqPairs q;
+  memset(&q, 0, sizeof q);
+  q.n = n;
+  for (int i = 0; i < n; ++i) {
+    q.src[i] = src[i];
+    q.dst[i] = dst[i];
+  }
+  RP_TRY_LAUNCH_N("pages.fork_plan", rp::launch_fork_plan(s, a, q, missing));
+  RP_TRY_LAUNCH_N("pages.fork_rows", rp::launch_fork_rows(s, a, q, missing));
+  return RP_OK;
+}
+
+rp_status rp_pages_free(const rp_pages* pages, void* stream, int32_t n, const int32_t* seqs) {
+  rp_status st = check_pages(pages);
+  if (st != RP_OK || (st = check_seqs(*pages, n, seqs, "seqs", true)) != RP_OK) return st;
+  hipStream_t s = (hipStream_t)stream;
+  rp::SeqRows q;
+  memset(&q, 0, sizeof q);
+  q.n = n;
+  for (int i = 0; i < n; ++i) q.seq[i] = seqs[i];
+  RP_TRY_LAUNCH_N("pages.free", rp::launch_pages_free(s, page_args(*pages), q));
+  return RP_OK;
+}
+
+rp_status rp_pages_compact_workspace_bytes(const rp_pages* pages, size_t* bytes) {
+  if (!bytes) return fail(RP_ERR_INVALID_ARG, "bytes is required");
+  const rp_status st = check_pages(pages);
+  if (st != RP_OK) return st;
+  *bytes = rp::compact_words(pages->n_pages) * 4;
+  return RP_OK;
+}
+
+rp_status rp_pages_compact(const rp_pages* pages, void* stream, int32_t* n_live, void* ws, size_t ws_bytes) {
+  rp_status st = check_pages(pages);
+  if (st != RP_OK || (st = check_ws(ws, ws_bytes, rp::compact_words(pages->n_pages) * 4)) != RP_OK) return st;
+  hipStream_t s = (hipStream_t)stream;
+  const rp::PageArgs a = page_args(*pages);
+  RP_TRY_LAUNCH_N("pages.compact_plan", rp::launch_compact_plan(s, a, n_live, (int32_t*)ws));
+  RP_TRY_LAUNCH_N("pages.compact_move", rp::launch_compact_move(s, a, (const int32_t*)ws));
+  return RP_OK;
+}
+
+rp_status rp_tree_attention_workspace_bytes(const rp_pages* pages, int32_t B, int32_t N, int32_t Hq, size_t* bytes) {
+  if (!bytes) return fail(RP_ERR_INVALID_ARG, "bytes is required");
+  rp_status st = check_pages(pages);
+  if (st != RP_OK || (st = check_tree(*pages, B, N)) != RP_OK || (st = check_tree_heads(*pages, Hq)) != RP_OK) return st;
+  *bytes = tree_attn_ws(pages->dtype, B, N, Hq, pages->n_kv_heads, pages->head_dim, nullptr, nullptr);
+  return RP_OK;
+}
+
+rp_status rp_tree_attention(const rp_pages* pages, void* stream, int32_t layer, int32_t B, int32_t N, int32_t Hq,
+                            const int32_t* n_nodes, const uint32_t* mask, const void* q, int64_t q_ld, const void* k_new,
+                            const void* v_new, float scale, void* out, void* ws, size_t ws_bytes) {
+  rp_status st = check_pages(pages);
+  if (st != RP_OK || (st = check_tree(*pages, B, N)) != RP_OK || (st = check_tree_heads(*pages, Hq)) != RP_OK) return st;
+  if (layer < 0 || layer >= pages->n_layers) return fail(RP_ERR_SHAPE, "layer %d outside [0, %d)", layer, pages->n_layers);
+  if (!q || !k_new || !v_new || !out) return fail(RP_ERR_INVALID_ARG, "q, k_new, v_new and out are required");
+  if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(out))
+    return fail(RP_ERR_INVALID_ARG, "q, k_new, v_new and out must be 16-byte aligned");
+  if (q_ld < (int64_t)Hq * pages->head_dim || q_ld % 8)
+    return fail(RP_ERR_SHAPE, "q_ld %lld: at least n_q_heads*head_dim = %lld, a multiple of 8", (long long)q_ld,
+                (long long)Hq * pages->head_dim);
+  if (!isfinite(scale)) return fail(RP_ERR_SHAPE, "scale must be finite");
+  const size_t need = tree_attn_ws(pages->dtype, B, N, Hq, pages->n_kv_heads, pages->head_dim, nullptr, nullptr);
+  if ((st = check_ws(ws, ws_bytes, need)) != RP_OK) return st;
+  hipStream_t s = (hipStream_t)stream;
+  rp::TreeArgs a = tree_args(*pages, B, N, Hq, n_nodes, mask);
+  tree_attn_ws(pages->dtype, B, N, Hq, pages->n_kv_heads, pages->head_dim, ws, &a.part);
+  DebugPass dbg;
+  if ((st = dbg.begin(s, ws)) != RP_OK) return st;
+  const int64_t at = layer * pages->kv.layer_stride * pages_elem(*pages);
+  a.q = q;
+  a.q_ld = q_ld;
+  a.k = (const char*)pages->kv.k + at;
+  a.v = (const char*)pages->kv.v + at;
+  a.kn = k_new;
+  a.vn = v_new;
+  a.out = out;
+  a.scale = scale;
+  RP_TRY_LAUNCH_N("tree.attention", rp::launch_tree_attention(s, pages->dtype, a));
+  return dbg.end(RP_OK);
+}
+
+rp_status rp_tree_step_workspace_bytes(const rp_model* m, int32_t B, int32_t N, size_t* bytes) {
+  if (!m || !bytes) return fail(RP_ERR_INVALID_ARG, "model and bytes are required");
+  if (B < 1 || N < 1 || N > RP_MAX_NODES) return fail(RP_ERR_SHAPE, "batch %d, new tokens %d outside [1, %d]", B, N, RP_MAX_NODES);
+  if ((int64_t)B * N > 1 << 24) return fail(RP_ERR_UNSUPPORTED, "batch * new tokens exceeds 2^24");
+  *bytes = tree_ws(m, B, N, nullptr, nullptr);
+  return RP_OK;
+}
+
+rp_status rp_tree_step(const rp_model* m, void* stream, const rp_pages* pages, int32_t B, int32_t N, const int32_t* n_nodes,
+                       const int32_t* token_ids, const int32_t* parents, const int32_t* pos0, rp_kv draft, float* logits,
+                       int32_t* next_ids, void* ws, size_t ws_bytes) {
+  if (!m) return fail(RP_ERR_INVALID_ARG, "model is NULL");
+  rp_status st = check_pages(pages);
+  if (st != RP_OK || (st = check_tree(*pages, B, N)) != RP_OK) return st;
+  const rp_config& c = m->cfg;
+  if (pages->dtype != c.dtype || pages->n_layers != c.n_layers || pages->n_kv_heads != c.n_kv_heads || pages->head_dim != c.head_dim)
+    return fail(RP_ERR_SHAPE, "pages: type, layers and heads must be the model's");
+  if (c.dtype == RP_BF16 && c.head_dim == 64)
+    return fail(RP_ERR_UNSUPPORTED, "rp_tree_step is disabled for bf16 models at head_dim 64, as rp_decode_step is");
+  const int64_t R = (int64_t)B * N;
+  if ((st = check_rows(*pages, draft, R, "draft")) != RP_OK) return st;
+  if (!token_ids || !next_ids) return fail(RP_ERR_INVALID_ARG, "token_ids and next_ids are required");
+  if (logits && !aligned16(logits)) return fail(RP_ERR_INVALID_ARG, "logits must be 16-byte aligned");
+  if ((st = check_ws(ws, ws_bytes, tree_ws(m, B, N, nullptr, nullptr))) != RP_OK) return st;
+
+  hipStream_t s = (hipStream_t)stream;
+  const rp_dtype dt = c.dtype;
+  const int d = c.d_model;
+  TreeWS w;
+  tree_ws(m, B, N, ws, &w);
+  DebugPass dbg;
+  if ((st = dbg.begin(s, ws)) != RP_OK) return st;
+  if (!n_nodes && (st = dbg.check_ids(token_ids, (int32_t)R, 0, c.vocab, "token_ids", rp::DBG_ID_RANGE)) != RP_OK) return st;
+  rp::TreeArgs tree = tree_args(*pages, B, N, c.n_q_heads, n_nodes, w.mask);
+  tree.q_ld = (int64_t)c.n_q_heads * c.head_dim;
+  tree.scale = (float)(1.0 / sqrt((double)c.head_dim));
+  tree.part = w.attn_part;
+  tree.zero_rest = true;
+  RP_TRY_LAUNCH_N("tree.plan", rp::launch_tree_plan(s, B, N, tree.W, parents, pos0, pages->len, c.max_position, w.mask,
+                                                    w.positions));
+  RP_TRY_LAUNCH_N("tree.embed_norm", rp::launch_decode_embed_norm(s, dt, token_ids, m->embed, c.vocab, (int32_t)R, d, w.L.X,
+                                                                  m->layers[0].attn_norm, c.rms_eps, w.L.N));
+  rp::SeqTable none;  // the rows' positions are w.positions
+  memset(&none, 0, sizeof none);
+  const rp::MRope mr = {w.positions, c.head_dim / 2, c.head_dim / 2};
+  bool normed = true;
+  for (int l = 0; l < c.n_layers; ++l) {
+    const void* next_norm = l + 1 < c.n_layers ? m->layers[l + 1].attn_norm : m->final_norm;
+    bool next = false;
+    st = run_layer(m, s, m->layers[l], none, (int32_t)R, w.L, layer_ptr(m, draft.k, draft.layer_stride, l),
+                   layer_ptr(m, draft.v, draft.layer_stride, l), layer_ptr(m, pages->kv.k, pages->kv.layer_stride, l),
+                   layer_ptr(m, pages->kv.v, pages->kv.layer_stride, l), w.plan, w.gemm_part, kTreeNames, mr, normed, next_norm,
+                   &next, nullptr, &tree);
+    if (st != RP_OK) return st;
+    normed = next;
+  }
+  if (!normed) RP_TRY_LAUNCH_N("tree.rmsnorm", rp::launch_rmsnorm(s, dt, w.L.X, m->final_norm, c.rms_eps, (int32_t)R, d, w.L.N));
+  rp::BSeg blm = {m->lm_head, m->lm_head, m->lm_head, c.vocab, c.vocab};
+  if (w.arg_part) {
+    RP_TRY_LAUNCH_N("tree.gemm_lm_head_argmax", rp::launch_gemm_argmax(s, dt, (int32_t)R, c.vocab, d, w.L.N, d, blm, d, logits,
+                                                                       w.arg_part, next_ids));
+    return dbg.end(RP_OK);
+  }
+  float* lg = logits ? logits : w.logits;
+  RP_TRY_LAUNCH_N("tree.gemm_lm_head", rp::launch_gemm(s, dt, (int32_t)R, c.vocab, d, w.L.N, d, blm, d, lg, c.vocab,
+                                                       rp::EPI_STORE_F32, 1, nullptr));
+  RP_TRY_LAUNCH_N("tree.argmax", rp::launch_argmax(s, lg, (int32_t)R, c.vocab, next_ids));
+  return dbg.end(RP_OK);
+}
+
+rp_status rp_tree_commit(const rp_pages* pages, void* stream, int32_t B, int32_t N, const int32_t* n_nodes,
+                         const int32_t* token_ids, const int32_t* parents, const int32_t* next_ids, rp_kv draft,
+                         int32_t* accepted, int32_t* n_accepted, int32_t* token_out, int32_t* missing) {
+  rp_status st = check_pages(pages);
+  if (st != RP_OK || (st = check_tree(*pages, B, N)) != RP_OK) return st;
+  if (B > rp::kMaxCommit) return fail(RP_ERR_UNSUPPORTED, "batch %d > %d", B, rp::kMaxCommit);
+  if (!token_ids || !next_ids || !accepted || !n_accepted || !token_out || !missing)
+    return fail(RP_ERR_INVALID_ARG, "token_ids, next_ids, accepted, n_accepted, token_out and missing are required");
+  if ((st = check_rows(*pages, draft, (int64_t)B * N, "draft")) != RP_OK) return st;
+  hipStream_t s = (hipStream_t)stream;
+  const rp::PageArgs a = page_args(*pages);
+  RP_TRY_LAUNCH_N("tree.walk", rp::launch_tree_walk(s, B, N, n_nodes, token_ids, parents, next_ids, accepted, n_accepted, token_out));
+  RP_TRY_LAUNCH_N("tree.commit_plan", rp::launch_commit_plan(s, a, B, N, accepted, n_accepted, token_out, missing));
+  RP_TRY_LAUNCH_N("tree.commit_rows", rp::launch_commit_rows(s, a, B, N, accepted, n_accepted, draft.k, draft.v,
+                                                             draft.layer_stride * pages_elem(*pages)));
+  return RP_OK;
 }
 
 rp_status rp_profile_enable(int enable, int32_t max_launches) {

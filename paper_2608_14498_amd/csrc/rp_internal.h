@@ -314,4 +314,64 @@ hipError_t launch_decode_attention(hipStream_t s, rp_dtype dt, const void* q, in
                                    int32_t cap, int32_t max_pos, int32_t B, int32_t Hq, int32_t Hkv,
                                    int32_t D, float scale, float* partials, float* sums, int64_t sums_floats, void* o);
 
+// ---- key/value cache in pages (pages.hip) ----
+constexpr int kMaxCommit = 4096;  // sequences of one commit
+constexpr int kMaxNodes = 256;    // drafted tokens of one sequence
+struct PageArgs {
+  uint8_t *k, *v;       // layer l, slot s at l * layer_bytes + s * row_bytes
+  int64_t layer_bytes;
+  int32_t row_bytes, n_layers, n_pages, lg;  // page size 1 << lg
+  int32_t *table, *len, *refs;
+  int32_t n_seqs, table_ld;
+};
+// Host lists, passed by value: packed rows cu[i] .. cu[i+1]-1 belong to sequence seq[i].
+struct SeqRows {
+  int32_t n;
+  int32_t seq[RP_MAX_SEQS];
+  int32_t cu[RP_MAX_SEQS + 1];
+};
+struct SeqPairs {
+  int32_t n;
+  int32_t src[RP_MAX_SEQS], dst[RP_MAX_SEQS];
+};
+hipError_t launch_append_plan(hipStream_t s, const PageArgs& a, const SeqRows& q, int32_t* missing);
+hipError_t launch_append_rows(hipStream_t s, const PageArgs& a, const SeqRows& q, const void* k, const void* v,
+                              int64_t layer_bytes, const int32_t* missing);
+hipError_t launch_pages_free(hipStream_t s, const PageArgs& a, const SeqRows& q);
+hipError_t launch_fork_plan(hipStream_t s, const PageArgs& a, const SeqPairs& q, int32_t* missing);
+hipError_t launch_fork_rows(hipStream_t s, const PageArgs& a, const SeqPairs& q, const int32_t* missing);
+size_t compact_words(int32_t n_pages);  // int32 words of scratch
+hipError_t launch_compact_plan(hipStream_t s, const PageArgs& a, int32_t* n_live, int32_t* ws);
+hipError_t launch_compact_move(hipStream_t s, const PageArgs& a, const int32_t* ws);
+hipError_t launch_tree_walk(hipStream_t s, int32_t B, int32_t N, const int32_t* n_nodes, const int32_t* tokens,
+                            const int32_t* parents, const int32_t* chosen, int32_t* accepted, int32_t* n_accepted,
+                            int32_t* token_out);
+hipError_t launch_commit_plan(hipStream_t s, const PageArgs& a, int32_t B, int32_t N, int32_t* accepted, int32_t* n_accepted,
+                              int32_t* token_out, int32_t* missing);
+hipError_t launch_commit_rows(hipStream_t s, const PageArgs& a, int32_t B, int32_t N, const int32_t* accepted,
+                              const int32_t* n_accepted, const void* k, const void* v, int64_t layer_bytes);
+
+// ---- attention of drafted tokens over pages (tree_attention.hip) ----
+// Queries: row b * N + i of q (row stride q_ld), head h at column h * D.  Keys: the len[b] tokens in
+// sequence b's pages (one layer's pool k, v of rows [Hkv][D]) and the rows b * N + j, j < n_nodes[b],
+// of kn, vn that bit j of mask[(b * N + i) * W ..] names (NULL: j <= i).
+struct TreeArgs {
+  const void* q;
+  int64_t q_ld;
+  const void *k, *v, *kn, *vn;
+  const int32_t *table, *len, *n_nodes;
+  const uint32_t* mask;
+  void* out;     // [B * N][Hq * D]; rows past n_nodes[b] are left as they were, or 0 where zero_rest
+  float* part;   // tree_partial_floats
+  int32_t n_pages, lg, table_ld, B, N, W, Hq, Hkv, D;
+  float scale;
+  bool zero_rest;
+};
+size_t tree_partial_floats(rp_dtype dt, int32_t B, int32_t N, int32_t Hq, int32_t Hkv, int32_t D);
+hipError_t launch_tree_attention(hipStream_t s, rp_dtype dt, const TreeArgs& a);
+// Trees given by parents (NULL: chains): mask words of ancestors and the node itself, and rotary
+// positions pos0[b] (NULL: len[b]) + depth, three equal rows of B * N, clamped to [0, max_pos).
+hipError_t launch_tree_plan(hipStream_t s, int32_t B, int32_t N, int32_t W, const int32_t* parents, const int32_t* pos0,
+                            const int32_t* len, int32_t max_pos, uint32_t* mask, int32_t* positions);
+
 }  // namespace rp

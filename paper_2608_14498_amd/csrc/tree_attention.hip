@@ -2,9 +2,21 @@
 //
 // Row i of sequence b attends to the len[b] cached tokens and to the drafted tokens that its mask
 // names; softmax statistics and sums in fp32.  A row that sees nothing is 0.
+//
+// Per sequence and kv head the rows are (drafted token, q head of the group) pairs: N * G query rows
+// read one stream of keys and values, len tokens from pages and then the drafted ones.  The work of a
+// launch is the key tiles of all sequences in a row; the lengths are on the device, so each
+// workgroup sums the tiles itself and takes its equal, contiguous share of them: no host value bounds
+// the split, and mixed lengths load the workgroups evenly.  A share may end inside a sequence: such
+// pieces leave (max, sum, unnormalised o) records, which k_tree_merge joins.
+//
+// Keys and values are copied straight into LDS through buffer resources whose extent is the rows that
+// exist in the page (or among the drafted tokens): the rest of a tile reads as zeros.
 #include "attn_common.h"
 #include "device_common.h"
 #include "rp_internal.h"
+
+#include <type_traits>
 
 namespace rp {
 
@@ -23,69 +35,953 @@ __device__ __forceinline__ uint32_t tree_word(const TreeArgs& a, int b, int i, i
   const int there = n - 32 * w;
   return there >= 32 ? m : there <= 0 ? 0u : m & ((1u << there) - 1);
 }
+__device__ __forceinline__ int tree_page(const TreeArgs& a, int b, int token) {
+  return min(max(a.table[(int64_t)b * a.table_ld + (token >> a.lg)], 0), a.n_pages - 1);
+}
+
+// Key tiles of KT tokens of sequence b: those of its pages, then those of its drafted tokens.
+template <int KT>
+__device__ __forceinline__ int tree_tiles(const TreeArgs& a, int b) {
+  const int nn = tree_nodes(a, b);
+  return nn == 0 ? 0 : (tree_len(a, b) + KT - 1) / KT + (nn + KT - 1) / KT;
+}
+
+// Inclusive sum over the workgroup's threads; red holds NT / 64 values.
+template <int NT>
+__device__ __forceinline__ int64_t tree_scan(int64_t v, int64_t* red, int64_t* total) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t u = __shfl_up((long long)v, o, 64);
+    if (lane >= o) v += u;
+  }
+  __syncthreads();
+  if (lane == 63) red[w] = v;
+  __syncthreads();
+  int64_t sum = 0, before = 0;
+#pragma unroll
+  for (int i = 0; i < NT / 64; ++i) {
+    before += i < w ? red[i] : 0;
+    sum += red[i];
+  }
+  *total = sum;
+  return v + before;
+}
+
+// The launch's work as one row of tiles, shared out to `shares` workgroups (fewer where that would
+// leave one less than `least` tiles).
+struct TreeShares {
+  int64_t tiles;
+  int shares;
+  __device__ int64_t begin(int w) const { return tiles * w / shares; }
+  __device__ int owner(int64_t u) const { return (int)(((u + 1) * shares - 1) / tiles); }
+};
+
+// Finds the tile `pick(shares)` of the row: sequence *b, its tile *t.  All threads of the workgroup
+// call it; pick returns -1 for nothing to look for.
+template <int NT, int KT, class P>
+__device__ __forceinline__ TreeShares tree_find(const TreeArgs& a, int most, int least, P&& pick, int* b, int* t) {
+  __shared__ int64_t red[NT / 64];
+  __shared__ int at[2];
+  const int tid = threadIdx.x;
+  int64_t sum = 0, part, incl = 0;
+  int mine = 0;
+  for (int base = 0; base < a.B; base += NT) {
+    mine = base + tid < a.B ? tree_tiles<KT>(a, base + tid) : 0;
+    incl = sum + tree_scan<NT>(mine, red, &part);
+    sum += part;
+  }
+  TreeShares sh;
+  sh.tiles = sum;
+  const int64_t fit = sum / least;
+  sh.shares = fit < 1 ? 1 : fit < most ? (int)fit : most;
+  const int64_t u = sum > 0 ? pick(sh) : -1;
+  *b = *t = 0;
+  if (u < 0) return sh;
+  if (a.B > NT) {  // (the sums of the last round only are at hand: once more)
+    sum = 0;
+    for (int base = 0; base < a.B && sum <= u; base += NT) {
+      mine = base + tid < a.B ? tree_tiles<KT>(a, base + tid) : 0;
+      incl = sum + tree_scan<NT>(mine, red, &part);
+      if (incl > u && incl - mine <= u) {
+        at[0] = base + tid;
+        at[1] = (int)(u - (incl - mine));
+      }
+      sum += part;
+    }
+  } else if (incl > u && incl - mine <= u) {
+    at[0] = tid;
+    at[1] = (int)(u - (incl - mine));
+  }
+  __syncthreads();
+  *b = __builtin_amdgcn_readfirstlane(at[0]);
+  *t = __builtin_amdgcn_readfirstlane(at[1]);
+  return sh;
+}
+
+// Records: share w leaves at most two, of the piece that continues a sequence (slot 0) and of the one
+// that begins one it does not end (slot 1).  A record is o [rows][D], then (max in log2 units, sum)
+// pairs of the block's BQ rows.
+__host__ __device__ constexpr int tree_record(int BQ, int D) { return BQ * (D + 2); }
+__device__ __forceinline__ int64_t tree_record_at(const TreeArgs& a, int w, int slot, int g, int rb, int RB, int BQ) {
+  return ((((int64_t)w * 2 + slot) * a.Hkv + g) * RB + rb) * tree_record(BQ, a.D);
+}
+
+template <typename T16>
+__device__ __forceinline__ bool not_finite(uint32_t w) {  // either half of w
+  constexpr uint32_t e = std::is_same<T16, f16_t>::value ? 0x7c00u : 0x7f80u;
+  return (w & e) == e || (w >> 16 & e) == e;
+}
+template <typename T16>
+__device__ __forceinline__ uint4 flip_sign(uint4 v, uint32_t flip) {
+  return make_uint4(v.x ^ flip, v.y ^ flip, v.z ^ flip, v.w ^ flip);
+}
+
+// Drafted values that are not numbers: a weight of 0 would not keep them from rows that do not see
+// their token.  Rows that do see it take them here, as they are (their weight is positive);
+// the tile is then cleaned of them (tree_clean) and multiplied as any other.
+// vis: tokens key0 .. key0 + 31 that this lane's row sees; V rows of 8-element chunks swizzled by vswz.
+template <typename T16, int D>
+__device__ __forceinline__ void tree_odd_values(const T16* v, int key0, uint32_t vis, int fk, f32x16_t (&o)[D / 32]) {
+  typedef Half16<T16> H;
+  auto odd = [](float x, bool seen) { return seen && !(fabsf(x) <= 3.4028235e38f) ? x : 0.f; };
+#pragma unroll 1
+  for (int key = key0; key < key0 + 32; ++key) {
+    const bool seen = vis >> (key - key0) & 1;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const uint2 x = *reinterpret_cast<const uint2*>(v + key * D + ((db * 4 + c) ^ vswz<D>(key)) * 8 + 4 * fk);
+        o[db][4 * c] += odd(H::lo_f(x.x), seen);
+        o[db][4 * c + 1] += odd(H::hi_f(x.x), seen);
+        o[db][4 * c + 2] += odd(H::lo_f(x.y), seen);
+        o[db][4 * c + 3] += odd(H::hi_f(x.y), seen);
+      }
+  }
+}
+template <typename T16>
+__device__ __forceinline__ u32x4_t tree_clean(u32x4_t x) {
+  constexpr uint32_t e = std::is_same<T16, f16_t>::value ? 0x7c00u : 0x7f80u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if ((x[i] & e) == e) x[i] &= 0xffff0000u;
+    if ((x[i] >> 16 & e) == e) x[i] &= 0xffffu;
+  }
+  return x;
+}
+
+// The softmax step of KB blocks of 32 keys for the row of this lane: s raw scores in, weights out.
+// vis[kb]: the keys it sees (bit = key), where `some` (uniform) says that not every lane sees all.
+template <int DB, int KB>
+__device__ __forceinline__ void tree_softmax(f32x16_t (&s)[KB], bool some, const uint32_t (&vis)[KB], int fk, float c2, float& m,
+                                             float& l, f32x16_t (&o)[DB]) {
+  if (some) {
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        s[kb][e] = vis[kb] >> (4 * fk) >> (8 * (e >> 2) + (e & 3)) & 1 ? s[kb][e] : kLowest;
+  }
+  float mx = kLowest;
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[kb][e]);
+  mx = fmaxf(mx, __shfl_xor(mx, 32, kWave)) * c2;
+  // raised only where some lane's maximum grows by more than 2^kLazy: numerator and sum share it
+  if (__any(mx > m + kLazy)) {
+    const float mn = fmaxf(m, mx);
+    const float alpha = __builtin_amdgcn_exp2f(m - mn);
+    m = mn;
+    l *= alpha;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[db][e] *= alpha;
+  }
+  float sum = 0.f;
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      float p = __builtin_amdgcn_exp2f(fmaf(s[kb][e], c2, -m));
+      if (some) p = vis[kb] >> (4 * fk) >> (8 * (e >> 2) + (e & 3)) & 1 ? p : 0.f;
+      s[kb][e] = p;
+      sum += p;
+    }
+  l += sum;
+}
+
+// Four output values of a finished row.
+template <typename T16>
+__device__ __forceinline__ void tree_store4(T16* to, float4 v, float inv) {
+  typedef Half16<T16> H;
+  uint2 w;
+  w.x = H::pack2(v.x * inv, v.y * inv);
+  w.y = H::pack2(v.z * inv, v.w * inv);
+  *reinterpret_cast<uint2*>(to) = w;
+}
+__device__ __forceinline__ float tree_inv(float l) { return l == 0.f ? 0.f : 1.0f / l; }
 
 }  // namespace
 
-// One workgroup a (row, head): 256 keys at a time, a thread a key for the scores and a dimension of
-// every (256 / D)-th key for the values.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void k_tree_attn(TreeArgs a) {
-  __shared__ float qs[D], p[256], red[16], os[256];
-  const int tid = threadIdx.x;
-  const int h = blockIdx.x % a.Hq, g = h / (a.Hq / a.Hkv);
-  const int row = blockIdx.x / a.Hq, b = row / a.N, i = row % a.N;
-  const int nn = tree_nodes(a, b), n0 = tree_len(a, b);
-  T* out = (T*)a.out + ((int64_t)row * a.Hq + h) * D;
-  if (i >= nn) {
-    if (a.zero_rest && tid < D) stf(out + tid, 0.f);
-    return;
-  }
-  if (tid < D) qs[tid] = ldf((const T*)a.q + (int64_t)row * a.q_ld + h * D + tid) * a.scale;
-  const int64_t ld = (int64_t)a.Hkv * D;
-  auto offset = [&](int t) {  // of key t's row
-    int id = a.table[(int64_t)b * a.table_ld + (t >> a.lg)];
-    id = min(max(id, 0), a.n_pages - 1);
-    return (((int64_t)id << a.lg) + (t & ((1 << a.lg) - 1))) * ld + g * D;
-  };
-  float m = kLowest, l = 0.f, o = 0.f;
-  const int d = tid % D, part = tid / D;
-  for (int base = 0; base < n0 + nn; base += 256) {
-    __syncthreads();
-    const int t = base + tid, j = t - n0;
-    const bool seen = t < n0 || (j < nn && (tree_word(a, b, i, j >> 5, nn) >> (j & 31) & 1));
-    float s = 0.f;
-    if (seen) {
-      const T* k = t < n0 ? (const T*)a.k + offset(t) : (const T*)a.kn + ((int64_t)b * a.N + j) * ld + g * D;
-      for (int c = 0; c < D; c += 8) {
-        float x[8];
-        load8(k + c, x);
+// ------------------------------------------------------------------------------------
+// Up to 64 rows a kv head (one token, small trees): bound by reading the cache.  A workgroup's three
+// waves take the tiles of 32 keys in turn, each through an LDS ring of three stages of its own
+// (two tiles of 16 KB in flight a wave; no barrier inside a piece), and join their sums in LDS at the
+// piece's end.  S^T = K Q^T and O^T += V^T P^T with v_mfma_f32_32x32x16 as in the prefix kernel:
+// a lane holds one row's scores.  A wave's page ids are read 64 tiles ahead, a lane each.
+// ------------------------------------------------------------------------------------
+constexpr int TS_WAVES = 3;
+template <typename T16, int D, int QW, bool SMALL>
+__global__ __launch_bounds__(64 * TS_WAVES) void k_tree_stream(TreeArgs a, int shares, int least) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  typedef Half16<T16> H;
+  typedef typename H::V8 V8;
+  constexpr int KT = 32, CH = D / 8, KSTEPS = D / 16, DB = D / 32, NW = TS_WAVES;
+  constexpr int LOADS = KT * CH / 64;    // copies of a wave per matrix and tile
+  constexpr int GL = LOADS / 4;          // of 8 keys
+  constexpr int QPS = 2 * KT * CH / 64;  // 16-byte quads of a lane in one stage
+  static_assert(QW * DB * 4 + 1 <= 3 * QPS, "a wave's sums fit its stages");
+  __shared__ u32x4_t S0[NW][2 * KT * CH], S1[NW][2 * KT * CH], S2[NW][2 * KT * CH];  // K tile, V tile
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int fr = lane & 31, fk = lane >> 5;
+  const int g = blockIdx.x % a.Hkv, w = blockIdx.x / a.Hkv;
+  const int G = a.Hq / a.Hkv;
+  int b, t0;
+  const TreeShares sh = tree_find<64 * NW, KT>(
+      a, shares, least, [&](const TreeShares& s) { return w < s.shares ? s.begin(w) : (int64_t)-1; }, &b, &t0);
+  if (sh.tiles == 0 || w >= sh.shares) return;
+  int64_t left = sh.begin(w + 1) - sh.begin(w);
+
+  const uint32_t row_bytes = (uint32_t)a.Hkv * D * sizeof(T16);
+  uint32_t koff[LOADS], voff[LOADS];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s = fmaf(x[e], qs[c + e], s);
+  for (int j = 0; j < LOADS; ++j) {
+    const int slot = j * 64 + lane, key = slot / CH, cp = slot % CH, from = SMALL ? key & 7 : key;
+    koff[j] = (uint32_t)from * row_bytes + (uint32_t)((cp ^ kswz<D>(key)) * 16);
+    voff[j] = (uint32_t)from * row_bytes + (uint32_t)((cp ^ vswz<D>(key)) * 16);
+  }
+  // a negative scale is a positive one on queries of the other sign
+  const float c2 = fabsf(a.scale) * 1.4426950408889634f;
+  const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+  const int tr_p = lane & 15;
+  const int tr_key = fk * 4 + (tr_p >> 2);
+  const int tr_col = ((lane & 16) ? 16 : 0) + 4 * (tr_p & 3);
+
+  for (; left > 0; ++b, t0 = 0) {
+    const int n0 = __builtin_amdgcn_readfirstlane(tree_len(a, b)), nn = __builtin_amdgcn_readfirstlane(tree_nodes(a, b));
+    if (nn == 0) continue;
+    const int P0 = (n0 + KT - 1) / KT, nt = P0 + (nn + KT - 1) / KT;
+    const int t1 = __builtin_amdgcn_readfirstlane(t0 + (int)min((int64_t)(nt - t0), left)), rows = nn * G;
+    left -= t1 - t0;
+    // This wave's tiles are t0 + wave + NW i.  Of drafted tokens there are two tiles at most (N <= 64),
+    // next to each other, so a wave has one at most: td, which it takes first, where the one copy of
+    // the code for masks and odd values is.  Then its cached tiles.
+    const int td = max(P0, t0) + ((wave + t0 - max(P0, t0)) % NW + NW) % NW;
+    const int ahead = td < t1 ? 1 : 0;
+    const int own = (min(t1, P0) - t0 - wave + NW - 1) / NW;  // cached tiles (<= 0: none)
+    const int64_t row0 = (int64_t)b * a.N;
+    V8 qf[QW][KSTEPS];
+    uint32_t drafted[QW];
+#pragma unroll
+    for (int qi = 0; qi < QW; ++qi) {
+      const int r = qi * 32 + fr, i = r / G;
+      const bool is = r < rows;
+      const T16* qp = (const T16*)a.q + (row0 + i) * a.q_ld + (g * G + r - i * G) * D + fk * 8;
+#pragma unroll
+      for (int ks = 0; ks < KSTEPS; ++ks) {
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (is) v = flip_sign<T16>(*reinterpret_cast<const uint4*>(qp + ks * 16), flip);
+        qf[qi][ks] = H::as_v8(v);
+      }
+      drafted[qi] = is && ahead ? tree_word(a, b, i, td - P0, nn) : 0u;
+    }
+    f32x16_t o[QW][DB];
+    float m[QW], l[QW];
+#pragma unroll
+    for (int qi = 0; qi < QW; ++qi) {
+      m[qi] = kLowest;
+      l[qi] = 0.f;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[qi][db][e] = 0.f;
+    }
+
+    int lead = ahead;  // the drafted tile is still to do
+    for (int seg = 0; seg < own || lead; seg += 64) {
+      const int n = max(0, min(64, own - seg)), ts = t0 + wave + NW * seg;  // cached tiles ts + NW i, i < n
+      int pid[SMALL ? 4 : 1];
+#pragma unroll
+      for (int q = 0; q < (SMALL ? 4 : 1); ++q) {
+        const int token = min((ts + NW * lane) * KT + 8 * q, n0 - 1);
+        pid[q] = lane < n && token >= 0 ? tree_page(a, b, token) : 0;
+      }
+      // Copies the 32 tokens of cached tile i, or of the drafted tile (i < 0), into R; past the
+      // segment's tiles nothing (out of range: nothing is fetched), so that the compiler counts the
+      // copies exactly.
+      auto load = [&](u32x4_t* R, int i) __attribute__((always_inline)) {
+        const bool cached = i >= 0;
+        const int first = cached ? (ts + NW * i) * KT : (td - P0) * KT;
+        const int cnt = i < n ? min(KT, (cached ? n0 : nn) - first) : 0;
+        const char* kb = (const char*)(cached ? a.k : a.kn) + (int64_t)g * D * sizeof(T16);
+        const char* vb = (const char*)(cached ? a.v : a.vn) + (int64_t)g * D * sizeof(T16);
+#pragma unroll
+        for (int q = 0; q < (SMALL ? 4 : 1); ++q) {
+          const int page = __builtin_amdgcn_readlane(pid[q], i & 63), from = first + 8 * q;
+          const int64_t row = cached ? ((int64_t)page << a.lg) + (from & ((1 << a.lg) - 1)) : row0 + from;
+          const int c = SMALL ? min(8, cnt - 8 * q) : cnt;
+          const int ext = c > 0 ? (int)((uint32_t)(c - 1) * row_bytes + D * (uint32_t)sizeof(T16)) : 0;
+          const __amdgpu_buffer_rsrc_t rk =
+              __builtin_amdgcn_make_buffer_rsrc(uniform_ptr((void*)(kb + row * row_bytes)), 0, __builtin_amdgcn_readfirstlane(ext), 0x00020000);
+          const __amdgpu_buffer_rsrc_t rv =
+              __builtin_amdgcn_make_buffer_rsrc(uniform_ptr((void*)(vb + row * row_bytes)), 0, __builtin_amdgcn_readfirstlane(ext), 0x00020000);
+#pragma unroll
+          for (int j = q * GL; j < (SMALL ? (q + 1) * GL : LOADS); ++j) {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void_t*)(R + j * 64), 16, koff[j], 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void_t*)(R + KT * CH + j * 64), 16, voff[j], 0, 0, 0);
+          }
+        }
+      };
+      // FIRST: the tile that may be the drafted one.
+      auto tile = [&](u32x4_t* R, int i, auto first_) __attribute__((always_inline)) {
+        constexpr bool FIRST = decltype(first_)::value;
+        u32x4_t *Kc = R, *Vc = R + KT * CH;
+        f32x16_t s[QW][1];
+#pragma unroll
+        for (int ks = 0; ks < KSTEPS; ++ks) {
+          const V8 kf = __builtin_bit_cast(V8, Kc[fr * CH + ((ks * 2 + fk) ^ kswz<D>(fr))]);
+#pragma unroll
+          for (int qi = 0; qi < QW; ++qi) s[qi][0] = H::mma(kf, qf[qi][ks], ks == 0 ? f32x16_t{} : s[qi][0]);
+        }
+        // s[qi][0][e] = score(key 8(e/4) + 4 fk + e%4, row fr)
+        const bool cached = !FIRST || i >= 0;
+        const int there = n0 - (ts + NW * i) * KT;
+        const bool some = !cached || there < KT;
+        const uint32_t tail = there >= KT ? ~0u : (1u << (there & 31)) - 1;
+        const T16* vbase = reinterpret_cast<const T16*>(Vc);
+#pragma unroll
+        for (int qi = 0; qi < QW; ++qi) {
+          const uint32_t vis[1] = {cached ? tail : drafted[qi]};
+          tree_softmax<DB, 1>(s[qi], some, vis, fk, c2, m[qi], l[qi], o[qi]);
+        }
+        if (!cached) {
+          bool odd = false;
+#pragma unroll
+          for (int j = 0; j < LOADS; ++j) {
+            const u32x4_t x = Vc[j * 64 + lane];
+            odd |= not_finite<T16>(x[0]) || not_finite<T16>(x[1]) || not_finite<T16>(x[2]) || not_finite<T16>(x[3]);
+          }
+          if (__any(odd)) {
+#pragma unroll
+            for (int qi = 0; qi < QW; ++qi) tree_odd_values<T16, D>(vbase, 0, drafted[qi], fk, o[qi]);
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) Vc[j * 64 + lane] = tree_clean<T16>(Vc[j * 64 + lane]);
+          }
+        }
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+          V8 pf[QW];
+#pragma unroll
+          for (int qi = 0; qi < QW; ++qi) {
+            const f32x16_t& x = s[qi][0];
+            pf[qi] = H::as_v8(make_uint4(H::pack2(x[hh * 8 + 0], x[hh * 8 + 1]), H::pack2(x[hh * 8 + 2], x[hh * 8 + 3]),
+                                         H::pack2(x[hh * 8 + 4], x[hh * 8 + 5]), H::pack2(x[hh * 8 + 6], x[hh * 8 + 7])));
+          }
+          const int ka = hh * 16 + tr_key, kc = ka + 8;
+#pragma unroll
+          for (int db = 0; db < DB; ++db) {
+            const int col = db * 32 + tr_col;
+            const int ca = ((col >> 3) ^ vswz<D>(ka)) * 8 + (col & 7);
+            const int cc = ((col >> 3) ^ vswz<D>(kc)) * 8 + (col & 7);
+            const v4i16_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t*)(vbase + ka * D + ca));
+            const v4i16_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t*)(vbase + kc * D + cc));
+            const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
+            const V8 vf = H::as_v8(make_uint4(l2.x, l2.y, h2.x, h2.y));
+#pragma unroll
+            for (int qi = 0; qi < QW; ++qi) o[qi][db] = H::mma(vf, pf[qi], o[qi][db]);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      // Tile i is in stage (i + lead) % 3, refilled once read.  The first before the loop: its wait covers
+      // the register loads too (a loop entered with some pending would drain every copy).
+      const std::true_type first{};
+      const std::false_type later{};
+      const int i0 = -lead;
+      load(S0[wave], i0);
+      load(S1[wave], i0 + 1);
+      load(S2[wave], i0 + 2);
+      tile(S0[wave], i0, first);
+      load(S0[wave], i0 + 3);
+      for (int i = i0 + 1; i < n; i += 3) {
+        tile(S1[wave], i, later);
+        load(S1[wave], i + 3);
+        if (i + 1 < n) tile(S2[wave], i + 1, later);
+        load(S2[wave], i + 4);
+        if (i + 2 < n) tile(S0[wave], i + 2, later);
+        load(S0[wave], i + 5);
+      }
+      __builtin_amdgcn_s_waitcnt(0);  // the stages are free
+      lead = 0;
+    }
+
+    // ---- the waves' sums joined: quad k = (qi, db, c) holds dims db*32 + 8 c + 4 fk .. + 3 of row qi*32 + fr ----
+    auto quad = [&](int wv, int k) -> u32x4_t* {
+      u32x4_t* st = k < QPS ? S0[wv] : k < 2 * QPS ? S1[wv] : S2[wv];
+      return st + (k % QPS) * 64 + lane;
+    };
+#pragma unroll
+    for (int qi = 0; qi < QW; ++qi)
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const float4 v = make_float4(o[qi][db][4 * c], o[qi][db][4 * c + 1], o[qi][db][4 * c + 2], o[qi][db][4 * c + 3]);
+          *quad(wave, (qi * DB + db) * 4 + c) = __builtin_bit_cast(u32x4_t, v);
+        }
+    {
+      float4 v = make_float4(m[0], l[0], 0.f, 0.f);
+      if constexpr (QW == 2) {
+        v.z = m[1];
+        v.w = l[1];
+      }
+      *quad(wave, QW * DB * 4) = __builtin_bit_cast(u32x4_t, v);
+    }
+    __syncthreads();
+    float f[QW][NW], M[QW], L[QW];
+#pragma unroll
+    for (int qi = 0; qi < QW; ++qi) {
+      float mw[NW], lw[NW];
+      M[qi] = kLowest;
+#pragma unroll
+      for (int v = 0; v < NW; ++v) {
+        const float4 x = __builtin_bit_cast(float4, *quad(v, QW * DB * 4));
+        mw[v] = qi ? x.z : x.x;
+        lw[v] = qi ? x.w : x.y;
+        M[qi] = fmaxf(M[qi], mw[v]);
+      }
+      L[qi] = 0.f;
+#pragma unroll
+      for (int v = 0; v < NW; ++v) {
+        f[qi][v] = __builtin_amdgcn_exp2f(mw[v] - M[qi]);
+        L[qi] = fmaf(lw[v], f[qi][v], L[qi]);
+      }
+      L[qi] += __shfl_xor(L[qi], 32, kWave);
+    }
+    const bool whole = t0 == 0 && t1 == nt;
+    float* rec = a.part + tree_record_at(a, w, t0 == 0, g, 0, 1, 32 * QW);
+    for (int k = wave; k < QW * DB * 4; k += NW) {
+      const int qi = k / (DB * 4), dim = (k % (DB * 4)) / 4 * 32 + 8 * (k & 3) + 4 * fk, r = qi * 32 + fr;
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int v = 0; v < NW; ++v) {
+        const float4 y = __builtin_bit_cast(float4, *quad(v, k));
+        const float z = QW == 2 && qi ? f[QW - 1][v] : f[0][v];
+        x.x = fmaf(y.x, z, x.x);
+        x.y = fmaf(y.y, z, x.y);
+        x.z = fmaf(y.z, z, x.z);
+        x.w = fmaf(y.w, z, x.w);
+      }
+      if (r >= rows) continue;
+      if (whole) {
+        const int i = r / G;
+        tree_store4<T16>((T16*)a.out + ((row0 + i) * a.Hq + g * G + r - i * G) * D + dim, x, tree_inv(QW == 2 && qi ? L[QW - 1] : L[0]));
+      } else {
+        *reinterpret_cast<float4*>(rec + r * D + dim) = x;
       }
     }
-    float mx = wave_max(seen ? s : -INFINITY);
-    if ((tid & 63) == 0) red[tid >> 6] = mx;
-    __syncthreads();
-    mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-    const float mn = fmaxf(m, mx), alpha = expf(m - mn);
-    m = mn;
-    const float e = seen ? expf(s - m) : 0.f;
-    p[tid] = seen ? e : -1.f;
-    l = l * alpha + block_sum(e, red);
-    o *= alpha;
-    const int cnt = min(256, n0 + nn - base);
-    for (int c = part; c < cnt; c += 256 / D) {
-      if (p[c] < 0.f) continue;  // a key that is not seen, whatever its value
-      const int tk = base + c;
-      const T* v = tk < n0 ? (const T*)a.v + offset(tk) : (const T*)a.vn + ((int64_t)b * a.N + tk - n0) * ld + g * D;
-      o = fmaf(p[c], ldf(v + d), o);
+    if (!whole && wave == 0 && fk == 0) {
+#pragma unroll
+      for (int qi = 0; qi < QW; ++qi)
+        if (qi * 32 + fr < rows) *reinterpret_cast<float2*>(rec + 32 * QW * D + 2 * (qi * 32 + fr)) = make_float2(M[qi], L[qi]);
+    }
+    __syncthreads();  // the stages are free again
+  }
+#endif
+}
+
+// ------------------------------------------------------------------------------------
+// More rows (large trees): bound by the matrix cores.  Blocks of NW x 32 rows share 64-key tiles, the
+// next tile's copies in flight under the present one, as in the prefix kernel.  The row blocks of one
+// share of tiles run next to each other on one XCD, so that its L2 serves all but the first.
+// ------------------------------------------------------------------------------------
+template <typename T16, int D, int NW, bool SMALL>
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void k_tree_block(TreeArgs a, int shares, int least, int RB) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  typedef Half16<T16> H;
+  typedef typename H::V8 V8;
+  constexpr int BQ = NW * 32, KT = 64, CH = D / 8, KSTEPS = D / 16, DB = D / 32, KB = KT / 32;
+  constexpr int LOADS = KT * CH / (NW * 64), KW = KT / NW;  // a wave copies KW keys of a tile
+  constexpr int NG = SMALL ? KW / 8 : 1, GL = LOADS / NG;
+  static_assert(KW % 8 == 0 && LOADS % NG == 0, "whole groups of 8 keys");
+  __shared__ u32x4_t Ks0[KT * CH], Ks1[KT * CH], Vs0[KT * CH], Vs1[KT * CH];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int fr = lane & 31, fk = lane >> 5;
+  const int G = a.Hq / a.Hkv;
+  const int local = blockIdx.x >> 3, pair = local / RB * 8 + (blockIdx.x & 7), rb = local % RB;
+  const int g = pair % a.Hkv, w = pair / a.Hkv;
+  if (w >= shares) return;
+  int b, t0;
+  const TreeShares sh = tree_find<64 * NW, KT>(
+      a, shares, least, [&](const TreeShares& s) { return w < s.shares ? s.begin(w) : (int64_t)-1; }, &b, &t0);
+  if (sh.tiles == 0 || w >= sh.shares) return;
+  int64_t left = sh.begin(w + 1) - sh.begin(w);
+
+  const uint32_t row_bytes = (uint32_t)a.Hkv * D * sizeof(T16);
+  uint32_t koff[LOADS], voff[LOADS];
+#pragma unroll
+  for (int j = 0; j < LOADS; ++j) {
+    const int slot = (wave * LOADS + j) * 64 + lane, key = slot / CH, cp = slot % CH, from = (key - wave * KW) & (SMALL ? 7 : KW - 1);
+    koff[j] = (uint32_t)from * row_bytes + (uint32_t)((cp ^ kswz<D>(key)) * 16);
+    voff[j] = (uint32_t)from * row_bytes + (uint32_t)((cp ^ vswz<D>(key)) * 16);
+  }
+  const float c2 = fabsf(a.scale) * 1.4426950408889634f;
+  const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+  const int tr_p = lane & 15;
+  const int tr_key = fk * 4 + (tr_p >> 2);
+  const int tr_col = ((lane & 16) ? 16 : 0) + 4 * (tr_p & 3);
+
+  for (; left > 0; ++b, t0 = 0) {
+    const int n0 = __builtin_amdgcn_readfirstlane(tree_len(a, b)), nn = __builtin_amdgcn_readfirstlane(tree_nodes(a, b));
+    if (nn == 0) continue;
+    const int P0 = (n0 + KT - 1) / KT, nt = P0 + (nn + KT - 1) / KT;
+    const int t1 = __builtin_amdgcn_readfirstlane(t0 + (int)min((int64_t)(nt - t0), left)), rows = nn * G;
+    left -= t1 - t0;
+    if (rb * BQ >= rows) continue;
+    const int64_t row0 = (int64_t)b * a.N;
+    const int r = rb * BQ + wave * 32 + fr, ri = min(r, rows - 1) / G;  // (rows past the last repeat it)
+    V8 qf[KSTEPS];
+    {
+      const T16* qp = (const T16*)a.q + (row0 + ri) * a.q_ld + (g * G + min(r, rows - 1) - ri * G) * D + fk * 8;
+#pragma unroll
+      for (int ks = 0; ks < KSTEPS; ++ks) qf[ks] = H::as_v8(flip_sign<T16>(*reinterpret_cast<const uint4*>(qp + ks * 16), flip));
+    }
+    f32x16_t o[DB];
+    float m = kLowest, l = 0.f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[db][e] = 0.f;
+
+    // One tile from (Kc, Vc): cached tokens, `there` of them from its first on, or (DRAFT) drafted ones.
+    auto compute = [&](const u32x4_t* Kc, u32x4_t* Vc, int there, uint32_t d0, uint32_t d1, auto draft_) __attribute__((always_inline)) {
+      constexpr bool DRAFT = decltype(draft_)::value;
+      f32x16_t s[KB];
+#pragma unroll
+      for (int ks = 0; ks < KSTEPS; ++ks)
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+          const int key = kb * 32 + fr;
+          const V8 kf = __builtin_bit_cast(V8, Kc[key * CH + ((ks * 2 + fk) ^ kswz<D>(key))]);
+          s[kb] = H::mma(kf, qf[ks], ks == 0 ? f32x16_t{} : s[kb]);
+        }
+      uint32_t vis[KB] = {d0, d1};
+      if (!DRAFT) {
+        vis[0] = there >= 32 ? ~0u : (1u << (there & 31)) - 1;
+        vis[1] = there >= 64 ? ~0u : there <= 32 ? 0u : (1u << (there & 31)) - 1;
+      }
+      tree_softmax<DB, KB>(s, DRAFT || there < KT, vis, fk, c2, m, l, o);
+      const T16* vbase = reinterpret_cast<const T16*>(Vc);
+      if (DRAFT) {  // (every wave looks at the whole tile, so that all of them agree)
+        bool odd = false;
+#pragma unroll
+        for (int j = 0; j < KT * CH / 64; ++j) {
+          const u32x4_t x = Vc[j * 64 + lane];
+          odd |= not_finite<T16>(x[0]) || not_finite<T16>(x[1]) || not_finite<T16>(x[2]) || not_finite<T16>(x[3]);
+        }
+        if (__any(odd)) {
+          tree_odd_values<T16, D>(vbase, 0, vis[0], fk, o);
+          tree_odd_values<T16, D>(vbase, 32, vis[1], fk, o);
+          __syncthreads();
+#pragma unroll
+          for (int j = 0; j < LOADS; ++j) Vc[(wave * LOADS + j) * 64 + lane] = tree_clean<T16>(Vc[(wave * LOADS + j) * 64 + lane]);
+          __syncthreads();
+        }
+      }
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+          const f32x16_t& x = s[kb];
+          const V8 pf = H::as_v8(make_uint4(H::pack2(x[hh * 8 + 0], x[hh * 8 + 1]), H::pack2(x[hh * 8 + 2], x[hh * 8 + 3]),
+                                            H::pack2(x[hh * 8 + 4], x[hh * 8 + 5]), H::pack2(x[hh * 8 + 6], x[hh * 8 + 7])));
+          const int ka = kb * 32 + hh * 16 + tr_key, kc = ka + 8;
+#pragma unroll
+          for (int db = 0; db < DB; ++db) {
+            const int col = db * 32 + tr_col;
+            const int ca = ((col >> 3) ^ vswz<D>(ka)) * 8 + (col & 7);
+            const int cc = ((col >> 3) ^ vswz<D>(kc)) * 8 + (col & 7);
+            const v4i16_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t*)(vbase + ka * D + ca));
+            const v4i16_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t*)(vbase + kc * D + cc));
+            const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
+            o[db] = H::mma(H::as_v8(make_uint4(l2.x, l2.y, h2.x, h2.y)), pf, o[db]);
+          }
+        }
+    };
+    // Copies this wave's KW of the tokens from `first` on, of n (cached: in page pg[q] each 8 or all).
+    auto copy = [&](u32x4_t* Kd, u32x4_t* Vd, const void* kp, const void* vp, int first, int n, const int* pg) __attribute__((always_inline)) {
+      const char* kb = (const char*)kp + (int64_t)g * D * sizeof(T16);
+      const char* vb = (const char*)vp + (int64_t)g * D * sizeof(T16);
+#pragma unroll
+      for (int q = 0; q < NG; ++q) {
+        const int from = first + wave * KW + 8 * q;
+        const int64_t row = pg ? ((int64_t)pg[q] << a.lg) + (from & ((1 << a.lg) - 1)) : row0 + from;
+        const int c = min(SMALL ? 8 : KW, n - from);
+        const int ext = c > 0 ? (int)((uint32_t)(c - 1) * row_bytes + D * (uint32_t)sizeof(T16)) : 0;
+        const __amdgpu_buffer_rsrc_t rk =
+            __builtin_amdgcn_make_buffer_rsrc(uniform_ptr((void*)(kb + row * row_bytes)), 0, __builtin_amdgcn_readfirstlane(ext), 0x00020000);
+        const __amdgpu_buffer_rsrc_t rv =
+            __builtin_amdgcn_make_buffer_rsrc(uniform_ptr((void*)(vb + row * row_bytes)), 0, __builtin_amdgcn_readfirstlane(ext), 0x00020000);
+#pragma unroll
+        for (int j = q * GL; j < (q + 1) * GL; ++j) {
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void_t*)(Kd + (wave * LOADS + j) * 64), 16, koff[j], 0, 0, 0);
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void_t*)(Vd + (wave * LOADS + j) * 64), 16, voff[j], 0, 0, 0);
+        }
+      }
+    };
+    int pid[NG], seg = t0;  // page ids of this wave's tokens in tiles seg + lane
+    auto load_pages = [&](int first) {
+      seg = first;
+#pragma unroll
+      for (int q = 0; q < NG; ++q) {
+        const int token = min((seg + lane) * KT + wave * KW + 8 * q, n0 - 1);
+        pid[q] = seg + lane < min(t1, P0) && token >= 0 ? tree_page(a, b, token) : 0;
+      }
+    };
+    auto load = [&](u32x4_t* Kd, u32x4_t* Vd, int t) __attribute__((always_inline)) {
+      int pg[NG];
+#pragma unroll
+      for (int q = 0; q < NG; ++q) pg[q] = __builtin_amdgcn_readlane(pid[q], t - seg);
+      copy(Kd, Vd, a.k, a.v, t * KT, n0, pg);
+    };
+    // Drafted tiles first (in buffer 0), in the one copy of the code for masks and odd values; the cached
+    // ones then start from buffer 1.
+    const int te = min(t1, P0);
+    if (t0 < te) load_pages(t0);
+    for (int t = max(t0, P0); t < t1; ++t) {
+      const int d = t - P0;
+      const uint32_t d0 = tree_word(a, b, ri, 2 * d, nn), d1 = 2 * d + 1 < a.W ? tree_word(a, b, ri, 2 * d + 1, nn) : 0u;
+      copy(Ks0, Vs0, a.kn, a.vn, d * KT, nn, nullptr);
+      if (t + 1 == t1 && t0 < te) load(Ks1, Vs1, t0);
+      __syncthreads();
+      compute(Ks0, Vs0, 0, d0, d1, std::true_type{});
+      __syncthreads();
+    }
+    for (int from = t0; from < te; from += 64) {
+      const int se = min(te, from + 64);
+      if (from > t0) load_pages(from);
+      if (from > t0 || t1 <= P0) {
+        load(Ks1, Vs1, from);
+        __syncthreads();
+      }
+      auto tile = [&](const u32x4_t* Kc, u32x4_t* Vc, u32x4_t* Kn, u32x4_t* Vn, int t) __attribute__((always_inline)) {
+        if (t + 1 < se) load(Kn, Vn, t + 1);
+        compute(Kc, Vc, n0 - t * KT, 0u, 0u, std::false_type{});
+        __syncthreads();
+      };
+      int t = from;
+      for (; t + 2 <= se; t += 2) {
+        tile(Ks1, Vs1, Ks0, Vs0, t);
+        tile(Ks0, Vs0, Ks1, Vs1, t + 1);
+      }
+      if (t < se) tile(Ks1, Vs1, Ks0, Vs0, t);
+    }
+
+    // o[db][e] = O^T(dim db*32 + 8(e/4) + 4 fk + e%4, row r)
+    const float L = l + __shfl_xor(l, 32, kWave);
+    if (r < rows) {
+      const bool whole = t0 == 0 && t1 == nt;
+      float* rec = a.part + tree_record_at(a, w, t0 == 0, g, rb, RB, BQ);
+      T16* op = (T16*)a.out + ((row0 + ri) * a.Hq + g * G + r - ri * G) * D;
+      const int in = r - rb * BQ;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const float4 v = make_float4(o[db][4 * c], o[db][4 * c + 1], o[db][4 * c + 2], o[db][4 * c + 3]);
+          const int dim = db * 32 + 8 * c + 4 * fk;
+          if (whole)
+            tree_store4<T16>(op + dim, v, tree_inv(L));
+          else
+            *reinterpret_cast<float4*>(rec + in * D + dim) = v;
+        }
+      if (!whole && fk == 0) *reinterpret_cast<float2*>(rec + BQ * D + 2 * in) = make_float2(m, L);
     }
   }
-  os[tid] = o;
+#endif
+}
+
+// ------------------------------------------------------------------------------------
+// fp32 on the fp32 matrix cores (v_mfma_f32_32x32x2: exact products), blocks of 32 rows whose NW waves
+// take the tiles of 32 keys in turn, fragments straight from global memory as in the prefix's fp32
+// kernel, and join their sums in LDS.
+// ------------------------------------------------------------------------------------
+template <int D, int NW>
+__global__ __launch_bounds__(NW * 64) void k_tree_f32(TreeArgs a, int shares, int least, int RB) {
+  constexpr int KT = 32, NC = D / 8, DB = D / 32;
+  __shared__ float4 part[NW][DB * 4][64];
+  __shared__ float2 ml[NW][64];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int fr = lane & 31, fk = lane >> 5;
+  const int G = a.Hq / a.Hkv;
+  const int rb = blockIdx.x % RB, g = blockIdx.x / RB % a.Hkv, w = blockIdx.x / RB / a.Hkv;
+  int b, t0;
+  const TreeShares sh = tree_find<64 * NW, KT>(
+      a, shares, least, [&](const TreeShares& s) { return w < s.shares ? s.begin(w) : (int64_t)-1; }, &b, &t0);
+  if (sh.tiles == 0 || w >= sh.shares) return;
+  int64_t left = sh.begin(w + 1) - sh.begin(w);
+  const int64_t ld = (int64_t)a.Hkv * D;
+
+  for (; left > 0; ++b, t0 = 0) {
+    const int n0 = __builtin_amdgcn_readfirstlane(tree_len(a, b)), nn = __builtin_amdgcn_readfirstlane(tree_nodes(a, b));
+    if (nn == 0) continue;
+    const int P0 = (n0 + KT - 1) / KT, nt = P0 + (nn + KT - 1) / KT;
+    const int t1 = __builtin_amdgcn_readfirstlane(t0 + (int)min((int64_t)(nt - t0), left)), rows = nn * G;
+    left -= t1 - t0;
+    if (rb * 32 >= rows) continue;
+    const int64_t row0 = (int64_t)b * a.N;
+    const int r = rb * 32 + fr, rc = min(r, rows - 1), ri = rc / G;
+    float4 q[NC];
+    const float* qp = (const float*)a.q + (row0 + ri) * a.q_ld + (g * G + rc - ri * G) * D + 4 * fk;
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      q[j] = *reinterpret_cast<const float4*>(qp + 8 * j);
+      q[j] = make_float4(q[j].x * a.scale, q[j].y * a.scale, q[j].z * a.scale, q[j].w * a.scale);
+    }
+    // page of key fr of tile t (its last one past the end), and rows' places: lane 8 j holds the
+    // page of keys 8 j .. 8 j + 7
+    auto page_of = [&](int t) { return t < P0 ? tree_page(a, b, min(t * KT + fr, n0 - 1)) : 0; };
+    float4 kf[NC];
+    auto load_k = [&](int t, int page) {
+      const bool cached = t < P0;
+      const int first = cached ? t * KT : (t - P0) * KT, key = min(fr, (cached ? n0 : nn) - first - 1);
+      const int64_t row = cached ? ((int64_t)page << a.lg) + ((first + key) & ((1 << a.lg) - 1)) : row0 + first + key;
+      const float* kp = (const float*)(cached ? a.k : a.kn) + row * ld + g * D + 4 * fk;
+#pragma unroll
+      for (int j = 0; j < NC; ++j) kf[j] = *reinterpret_cast<const float4*>(kp + 8 * j);
+    };
+    f32x16_t o[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[db][e] = 0.f;
+    float m = kLowest, l = 0.f;
+    int page = 0, page_next = 0;
+    if (t0 + wave < t1) {
+      page = page_of(t0 + wave);
+      if (t0 + wave + NW < t1) page_next = page_of(t0 + wave + NW);
+      load_k(t0 + wave, page);
+    }
+    for (int t = t0 + wave; t < t1; t += NW) {
+      const bool cached = t < P0;
+      const int first = cached ? t * KT : (t - P0) * KT, cnt = min(KT, (cached ? n0 : nn) - first);
+      uint32_t vis = cnt >= 32 ? ~0u : (1u << cnt) - 1;
+      if (!cached) vis = tree_word(a, b, ri, t - P0, nn);
+      float vf[DB][16];
+      const float* vb = (const float*)(cached ? a.v : a.vn) + g * D;
+      auto v_row = [&](int key) {  // key 8 j + ..: the page is lane 8 j's
+        const int pg = __builtin_amdgcn_readlane(page, key & 24);
+        return cached ? ((int64_t)pg << a.lg) + ((first + (key & 24)) & ((1 << a.lg) - 1)) : row0 + first + (key & 24);
+      };
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int in = 4 * fk + (e & 3), key = 8 * (e >> 2) + in;
+        const bool is = key < cnt;
+        const float* vp = vb + (v_row(8 * (is ? (e >> 2) : 0)) + (is ? in : 0)) * ld + fr;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          const float x = vp[db * 32];
+          vf[db][e] = is ? x : 0.f;
+        }
+      }
+      f32x16_t s;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+      for (int j = 0; j < NC; ++j) {
+        s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[j].x, q[j].x, s, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[j].y, q[j].y, s, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[j].z, q[j].z, s, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[j].w, q[j].w, s, 0, 0, 0);
+      }
+      if (t + NW < t1) load_k(t + NW, page_next);
+      const uint32_t mine = vis >> (4 * fk);  // s[e]: key 8(e/4) + 4 fk + e%4
+      float mx = kLowest;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        s[e] = mine >> (8 * (e >> 2) + (e & 3)) & 1 ? s[e] : kLowest;
+        mx = fmaxf(mx, s[e]);
+      }
+      mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+      const float mn = fmaxf(m, mx), alpha = expf(m - mn);
+      m = mn;
+      l *= alpha;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[db][e] *= alpha;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        s[e] = mine >> (8 * (e >> 2) + (e & 3)) & 1 ? expf(s[e] - mn) : 0.f;
+        l += s[e];
+      }
+      bool odd = false;  // values that a weight of 0 would not keep away
+      if (!cached) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+#pragma unroll
+          for (int db = 0; db < DB; ++db) odd |= !(fabsf(vf[db][e]) <= 3.4028235e38f);
+      }
+      if (__any(odd)) {  // (as in tree_odd_values)
+#pragma unroll 1
+        for (int key = 0; key < cnt; ++key) {
+          const bool seen = vis >> key & 1;
+          const float* vp = (const float*)a.vn + (row0 + first + key) * ld + g * D + 4 * fk;
+#pragma unroll
+          for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int c = 0; c < 16; ++c) {
+              const float x = vp[db * 32 + 8 * (c >> 2) + (c & 3)];
+              o[db][c] += seen && !(fabsf(x) <= 3.4028235e38f) ? x : 0.f;
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+#pragma unroll
+          for (int db = 0; db < DB; ++db) vf[db][e] = fabsf(vf[db][e]) <= 3.4028235e38f ? vf[db][e] : 0.f;
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[db][e], s[e], o[db], 0, 0, 0);
+      page = page_next;
+      if (t + 2 * NW < t1) page_next = page_of(t + 2 * NW);
+    }
+    l += __shfl_xor(l, 32, kWave);
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        part[wave][db * 4 + c][lane] = make_float4(o[db][4 * c], o[db][4 * c + 1], o[db][4 * c + 2], o[db][4 * c + 3]);
+    ml[wave][lane] = make_float2(m, l);
+    __syncthreads();
+    float M = kLowest, L = 0.f, f[NW];
+#pragma unroll
+    for (int v = 0; v < NW; ++v) M = fmaxf(M, ml[v][lane].x);
+#pragma unroll
+    for (int v = 0; v < NW; ++v) {
+      f[v] = expf(ml[v][lane].x - M);
+      L = fmaf(ml[v][lane].y, f[v], L);
+    }
+    const bool whole = t0 == 0 && t1 == nt;
+    float* rec = a.part + tree_record_at(a, w, t0 == 0, g, rb, RB, 32);
+    const float inv = tree_inv(L);
+    for (int k = wave; k < DB * 4; k += NW) {
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int v = 0; v < NW; ++v) {
+        const float4 y = part[v][k][lane];
+        x.x = fmaf(y.x, f[v], x.x);
+        x.y = fmaf(y.y, f[v], x.y);
+        x.z = fmaf(y.z, f[v], x.z);
+        x.w = fmaf(y.w, f[v], x.w);
+      }
+      if (r >= rows) continue;
+      const int dim = (k >> 2) * 32 + 8 * (k & 3) + 4 * fk;
+      if (whole)
+        *reinterpret_cast<float4*>((float*)a.out + ((row0 + ri) * a.Hq + g * G + r - ri * G) * D + dim) =
+            make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
+      else
+        *reinterpret_cast<float4*>(rec + fr * D + dim) = x;
+    }
+    // (the fp32 kernel's maxima are natural logarithms: to log2 units for the merge)
+    if (!whole && wave == 0 && fk == 0 && r < rows)
+      *reinterpret_cast<float2*>(rec + 32 * D + 2 * fr) = make_float2(fmaxf(M * 1.4426950408889634f, kLowest), L);
+    __syncthreads();
+  }
+}
+
+// Joins the records of the sequences that several shares hold, one wave a row, shares in order; zeroes
+// the padding rows where asked.  One workgroup per (sequence, kv head, TM_ROWS rows).
+constexpr int TM_ROWS = 16;
+template <typename T, int D, int KT>
+__global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a, int most, int least, int BQ, int RB) {
+  constexpr int PER = D / 64;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int groups = (a.N * (a.Hq / a.Hkv) + TM_ROWS - 1) / TM_ROWS;
+  const int r0 = blockIdx.x % groups * TM_ROWS, g = blockIdx.x / groups % a.Hkv, b = blockIdx.x / groups / a.Hkv;
+  const int G = a.Hq / a.Hkv, nn = tree_nodes(a, b), rows = nn * G;
+  const int64_t row0 = (int64_t)b * a.N;
+  if (a.zero_rest) {
+    for (int r = max(r0, rows) + wave; r < min(r0 + TM_ROWS, a.N * G); r += 4) {
+      const int i = r / G;
+      T* op = (T*)a.out + ((row0 + i) * a.Hq + g * G + r - i * G) * D + lane * PER;
+#pragma unroll
+      for (int c = 0; c < PER; ++c) stf(op + c, 0.f);
+    }
+  }
+  if (r0 >= rows) return;
+  // tiles before this sequence, and of all
+  __shared__ int64_t red[8];
+  int64_t before = 0, all = 0;
+  for (int x = threadIdx.x; x < a.B; x += 256) {
+    const int n = tree_tiles<KT>(a, x);
+    all += n;
+    before += x < b ? n : 0;
+  }
+  before = wave_sum((long long)before);
+  all = wave_sum((long long)all);
+  if (lane == 0) {
+    red[wave] = before;
+    red[4 + wave] = all;
+  }
   __syncthreads();
-  if (tid >= D) return;
-  for (int c = 1; c < 256 / D; ++c) o += os[c * D + tid];
-  stf(out + tid, l == 0.f ? 0.f : o / l);
+  before = red[0] + red[1] + red[2] + red[3];
+  TreeShares sh;
+  sh.tiles = red[4] + red[5] + red[6] + red[7];
+  const int64_t fit = sh.tiles / least;
+  sh.shares = fit < 1 ? 1 : fit < most ? (int)fit : most;
+  const int wa = __builtin_amdgcn_readfirstlane(sh.owner(before));
+  const int wb = __builtin_amdgcn_readfirstlane(sh.owner(before + tree_tiles<KT>(a, b) - 1));
+  if (wa == wb) return;  // one share held it all
+  for (int r = r0 + wave; r < min(r0 + TM_ROWS, rows); r += 4) {
+    const int rb = r / BQ, in = r - rb * BQ;
+    auto record = [&](int w) { return a.part + tree_record_at(a, w, w == wa, g, rb, RB, BQ); };
+    float M = kLowest;
+    for (int w = wa + lane; w <= wb; w += 64) M = fmaxf(M, record(w)[BQ * D + 2 * in]);
+    M = wave_max(M);
+    float L = 0.f, o[PER] = {};
+    for (int base = wa; base <= wb; base += 64) {
+      const int w = base + lane;
+      float f = 0.f;
+      if (w <= wb) {
+        const float2 x = *reinterpret_cast<const float2*>(record(w) + BQ * D + 2 * in);
+        f = __builtin_amdgcn_exp2f(x.x - M);
+        L = fmaf(x.y, f, L);
+      }
+      const int n = min(64, wb - base + 1);
+#pragma unroll 4
+      for (int k = 0; k < n; ++k) {
+        const float z = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), k));
+        const float* x = record(base + k) + in * D + lane * PER;
+#pragma unroll
+        for (int c = 0; c < PER; ++c) o[c] = fmaf(x[c], z, o[c]);
+      }
+    }
+    const float inv = tree_inv(wave_sum(L));
+    const int i = r / G;
+    T* op = (T*)a.out + ((row0 + i) * a.Hq + g * G + r - i * G) * D + lane * PER;
+#pragma unroll
+    for (int c = 0; c < PER; ++c) stf(op + c, o[c] * inv);
+  }
 }
 
 // One workgroup a sequence, thread i node i: ancestors by walking up.  A parent outside [0, i) is none.
@@ -118,16 +1014,73 @@ __global__ __launch_bounds__(kMaxNodes) void k_tree_plan(int N, int W, const int
   positions[2 * rows + row] = pos;
 }
 
-size_t tree_partial_floats(rp_dtype, int32_t, int32_t, int32_t, int32_t, int32_t) { return 0; }
+// How a launch runs: rows of a block, row blocks, shares of the tiles (a share: one workgroup per kv head
+// and row block) and the least tiles of one.
+struct TreePlan {
+  bool stream;
+  int BQ, RB, shares, least;
+};
+static TreePlan tree_plan(rp_dtype dt, int32_t N, int32_t Hq, int32_t Hkv) {
+  TreePlan p;
+  const int rows = N * (Hq / Hkv);
+  p.stream = dt != RP_F32 && rows <= 64;
+  p.BQ = dt == RP_F32 ? 32 : p.stream ? (rows <= 32 ? 32 : 64) : 128;
+  p.RB = (rows + p.BQ - 1) / p.BQ;
+  // a stream workgroup has a CU's LDS to itself, of the others two share one
+  p.shares = (p.stream ? 256 : 512) / (Hkv * p.RB);
+  if (p.shares < 1) p.shares = 1;
+  p.least = p.stream ? 3 : 4;
+  return p;
+}
+
+size_t tree_partial_floats(rp_dtype dt, int32_t, int32_t N, int32_t Hq, int32_t Hkv, int32_t D) {
+  const TreePlan p = tree_plan(dt, N, Hq, Hkv);
+  return (size_t)p.shares * 2 * Hkv * p.RB * tree_record(p.BQ, D);
+}
 
 hipError_t launch_tree_attention(hipStream_t s, rp_dtype dt, const TreeArgs& a) {
-  with_storage(dt, [&](auto tag_) {
+  const TreePlan p = tree_plan(dt, a.N, a.Hq, a.Hkv);
+  typedef std::integral_constant<int, 128> D128;
+  typedef std::integral_constant<int, 64> D64;
+  const int merge = (a.N * (a.Hq / a.Hkv) + TM_ROWS - 1) / TM_ROWS * a.Hkv * a.B;
+  if (dt == RP_F32) {
+    const int grid = p.shares * a.Hkv * p.RB;
+    if (a.D == 128) {
+      k_tree_f32<128, 4><<<grid, 256, 0, s>>>(a, p.shares, p.least, p.RB);
+      k_tree_merge<float, 128, 32><<<merge, 256, 0, s>>>(a, p.shares, p.least, p.BQ, p.RB);
+    } else {
+      k_tree_f32<64, 8><<<grid, 512, 0, s>>>(a, p.shares, p.least, p.RB);
+      k_tree_merge<float, 64, 32><<<merge, 256, 0, s>>>(a, p.shares, p.least, p.BQ, p.RB);
+    }
+    return hipGetLastError();
+  }
+  with_half16(dt, [&](auto tag_) {
     using T = decltype(tag_);
-    const int grid = a.B * a.N * a.Hq;
+    auto run = [&](auto d_) {
+      constexpr int D = decltype(d_)::value;
+      if (p.stream) {
+        const int grid = p.shares * a.Hkv;
+        const bool small = a.lg < 5;
+        if (p.BQ == 32)
+          small ? k_tree_stream<T, D, 1, true><<<grid, 64 * TS_WAVES, 0, s>>>(a, p.shares, p.least)
+                : k_tree_stream<T, D, 1, false><<<grid, 64 * TS_WAVES, 0, s>>>(a, p.shares, p.least);
+        else
+          small ? k_tree_stream<T, D, 2, true><<<grid, 64 * TS_WAVES, 0, s>>>(a, p.shares, p.least)
+                : k_tree_stream<T, D, 2, false><<<grid, 64 * TS_WAVES, 0, s>>>(a, p.shares, p.least);
+        k_tree_merge<T, D, 32><<<merge, 256, 0, s>>>(a, p.shares, p.least, p.BQ, p.RB);
+      } else {
+        const int grid = (p.shares * a.Hkv + 7) / 8 * 8 * p.RB;
+        if (a.lg < 4)
+          k_tree_block<T, D, 4, true><<<grid, 256, 0, s>>>(a, p.shares, p.least, p.RB);
+        else
+          k_tree_block<T, D, 4, false><<<grid, 256, 0, s>>>(a, p.shares, p.least, p.RB);
+        k_tree_merge<T, D, 64><<<merge, 256, 0, s>>>(a, p.shares, p.least, p.BQ, p.RB);
+      }
+    };
     if (a.D == 128)
-      k_tree_attn<T, 128><<<grid, 256, 0, s>>>(a);
+      run(D128{});
     else
-      k_tree_attn<T, 64><<<grid, 256, 0, s>>>(a);
+      run(D64{});
   });
   return hipGetLastError();
 }

@@ -26,6 +26,9 @@ LIBDIR = os.path.join(PKG, "lib")
 LIB = os.path.join(LIBDIR, "librollplex.so")
 SOURCES = ["api.cpp", "elementwise.hip", "gemm.hip", "gemm_flex.hip", "attention.hip", "calibrate.hip",
            "pages.hip", "tree_attention.hip"]
+# MFMA results in ordinary registers: kernels whose softmax works on every result would otherwise
+# move each of them out of accumulation registers first.
+SOURCE_FLAGS = {"tree_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
@@ -60,7 +63,7 @@ def build(verbose: bool = False, sanitize: bool = False) -> str:
     for src in SOURCES:
         obj = os.path.join(objdir, src.replace(".", "_") + ".o")
         lang = ["-x", "hip"] if src.endswith(".cpp") else []
-        jobs.append([HIPCC] + FLAGS + extra + lang + ["-c", os.path.join(CSRC, src), "-o", obj])
+        jobs.append([HIPCC] + FLAGS + SOURCE_FLAGS.get(src, []) + extra + lang + ["-c", os.path.join(CSRC, src), "-o", obj])
         objs.append(obj)
     with ThreadPoolExecutor(min(8, len(jobs))) as ex:
         list(ex.map(lambda c: _run(c, verbose), jobs))

@@ -363,9 +363,11 @@ struct TreeArgs {
   const uint32_t* mask;
   void* out;     // [B * N][Hq * D]; rows past n_nodes[b] are left as they were, or 0 where zero_rest
   float* part;   // tree_partial_floats
+  int2* held;    // (set by launch_tree_attention: inside part) first and last share of every sequence
   int32_t n_pages, lg, table_ld, B, N, W, Hq, Hkv, D;
   float scale;
   bool zero_rest;
+  bool few;  // (set by launch_tree_attention) at most 64 sequences, whose tiles together fit an int
 };
 size_t tree_partial_floats(rp_dtype dt, int32_t B, int32_t N, int32_t Hq, int32_t Hkv, int32_t D);
 hipError_t launch_tree_attention(hipStream_t s, rp_dtype dt, const TreeArgs& a);

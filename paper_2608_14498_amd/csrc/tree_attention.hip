@@ -68,54 +68,99 @@ __device__ __forceinline__ int64_t tree_scan(int64_t v, int64_t* red, int64_t* t
   return v + before;
 }
 
-// The launch's work as one row of tiles, shared out to `shares` workgroups (fewer where that would
-// leave one less than `least` tiles).
+// The launch's work as one row of tiles, shared out to at most `most` shares of at least `least` tiles.
+// chunk > 0: each sequence is cut into shares of its own, of `chunk` tiles (the last of it may be
+// smaller); else the row is cut evenly and a share may end one sequence and begin the next.
 struct TreeShares {
   int64_t tiles;
-  int shares;
+  int shares, chunk;
   __device__ int64_t begin(int w) const { return tiles * w / shares; }
   __device__ int owner(int64_t u) const { return (int)(((u + 1) * shares - 1) / tiles); }
 };
+struct TreePiece {  // where a share begins and how many tiles it has (none: left = 0)
+  int b, t;
+  int64_t left;
+};
 
-// Finds the tile `pick(shares)` of the row: sequence *b, its tile *t.  All threads of the workgroup
-// call it; pick returns -1 for nothing to look for.
-template <int NT, int KT, class P>
-__device__ __forceinline__ TreeShares tree_find(const TreeArgs& a, int most, int least, P&& pick, int* b, int* t) {
+// The shares that hold sequence b, for the merge, written by the one that begins it; `first`: its first tile
+// in the row.
+__device__ __forceinline__ void tree_note(const TreeArgs& a, const TreeShares& sh, int b, int w, int64_t first, int nt) {
+  if (threadIdx.x == 0) a.held[b] = make_int2(w, sh.chunk ? w + (nt + sh.chunk - 1) / sh.chunk - 1 : sh.owner(first + nt - 1));
+}
+
+// Share w.  All threads of the workgroup call it.  Up to 64 sequences are cut into chunks of their own
+// where that makes a share at most `slack` tiles longer than an even cut: a second piece costs a
+// share its queries, page ids and first tiles all over again, one after the other.  8 sequences of 300 to
+// 1000 keys, 4 kv heads of 128: 18.2 us evenly cut, CHUNKED_US in chunks.
+template <int NT, int KT>
+__device__ __forceinline__ TreeShares tree_find(const TreeArgs& a, int most, int least, int slack, int w, TreePiece* p) {
   __shared__ int64_t red[NT / 64];
   __shared__ int at[2];
+  p->b = p->t = 0;
+  p->left = 0;
+  auto even = [&](int64_t tiles) {
+    const int64_t fit = tiles / least;
+    return TreeShares{tiles, fit < 1 ? 1 : fit < most ? (int)fit : most, 0};
+  };
+  if (a.few) {  // every wave by itself, a sequence a lane
+    const int lane = threadIdx.x & 63;
+    const int mine = lane < a.B ? tree_tiles<KT>(a, lane) : 0;
+    auto scan = [&](int v) {
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int x = __shfl_up(v, o, 64);
+        if (lane >= o) v += x;
+      }
+      return v;
+    };
+    const int incl = scan(mine), total = __builtin_amdgcn_readlane(incl, 63);
+    TreeShares sh = even(total);
+    const int ideal = (total + sh.shares - 1) / sh.shares;
+    for (int c = ideal; c <= ideal + slack && total > 0; c += 1 + c / 16) {
+      const int cuts = (mine + c - 1) / c, ci = scan(cuts), n = __builtin_amdgcn_readlane(ci, 63);
+      if (n > most) continue;
+      sh.shares = n;
+      sh.chunk = c;
+      const uint64_t past = __ballot(ci > w);
+      if (past) {
+        p->b = __builtin_ctzll(past);
+        p->t = (w - __builtin_amdgcn_readlane(ci - cuts, p->b)) * c;
+        p->left = min(c, __builtin_amdgcn_readlane(mine, p->b) - p->t);
+      }
+      return sh;
+    }
+    if (total == 0 || w >= sh.shares) return sh;
+    const int u = (int)sh.begin(w);
+    p->b = __builtin_ctzll(__ballot(incl > u));
+    p->t = u - __builtin_amdgcn_readlane(incl - mine, p->b);
+    p->left = sh.begin(w + 1) - u;
+    return sh;
+  }
   const int tid = threadIdx.x;
   int64_t sum = 0, part, incl = 0;
   int mine = 0;
   for (int base = 0; base < a.B; base += NT) {
     mine = base + tid < a.B ? tree_tiles<KT>(a, base + tid) : 0;
-    incl = sum + tree_scan<NT>(mine, red, &part);
+    tree_scan<NT>(mine, red, &part);
     sum += part;
   }
-  TreeShares sh;
-  sh.tiles = sum;
-  const int64_t fit = sum / least;
-  sh.shares = fit < 1 ? 1 : fit < most ? (int)fit : most;
-  const int64_t u = sum > 0 ? pick(sh) : -1;
-  *b = *t = 0;
-  if (u < 0) return sh;
-  if (a.B > NT) {  // (the sums of the last round only are at hand: once more)
-    sum = 0;
-    for (int base = 0; base < a.B && sum <= u; base += NT) {
-      mine = base + tid < a.B ? tree_tiles<KT>(a, base + tid) : 0;
-      incl = sum + tree_scan<NT>(mine, red, &part);
-      if (incl > u && incl - mine <= u) {
-        at[0] = base + tid;
-        at[1] = (int)(u - (incl - mine));
-      }
-      sum += part;
+  const TreeShares sh = even(sum);
+  if (sum == 0 || w >= sh.shares) return sh;
+  const int64_t u = sh.begin(w);
+  sum = 0;
+  for (int base = 0; base < a.B && sum <= u; base += NT) {
+    mine = base + tid < a.B ? tree_tiles<KT>(a, base + tid) : 0;
+    incl = sum + tree_scan<NT>(mine, red, &part);
+    if (incl > u && incl - mine <= u) {
+      at[0] = base + tid;
+      at[1] = (int)(u - (incl - mine));
     }
-  } else if (incl > u && incl - mine <= u) {
-    at[0] = tid;
-    at[1] = (int)(u - (incl - mine));
+    sum += part;
   }
   __syncthreads();
-  *b = __builtin_amdgcn_readfirstlane(at[0]);
-  *t = __builtin_amdgcn_readfirstlane(at[1]);
+  p->b = __builtin_amdgcn_readfirstlane(at[0]);
+  p->t = __builtin_amdgcn_readfirstlane(at[1]);
+  p->left = sh.begin(w + 1) - u;
   return sh;
 }
 
@@ -171,17 +216,27 @@ __device__ __forceinline__ u32x4_t tree_clean(u32x4_t x) {
   return x;
 }
 
+// A score, or the lowest where it is not seen.  The empty asm keeps a branch around it a branch: the
+// compiler would mask all scores of all tiles instead, most of which are whole.
+__device__ __forceinline__ float tree_masked(float s, bool seen) {
+  s = seen ? s : kLowest;
+  asm volatile("" : "+v"(s));
+  return s;
+}
+
 // The softmax step of KB blocks of 32 keys for the row of this lane: s raw scores in, weights out.
-// vis[kb]: the keys it sees (bit = key), where `some` (uniform) says that not every lane sees all.
-template <int DB, int KB>
+// vis[kb]: the keys it sees (bit = key).  TAIL: cached tokens, where `some` (uniform) says that the tile
+// is not full; every row sees its first key, so a masked score's weight is 0 by itself.  DRAFT: a row
+// may see nothing, and weights are cleared one by one.
+enum TreeMask { kTail, kDraft };
+template <int DB, int KB, TreeMask MASK>
 __device__ __forceinline__ void tree_softmax(f32x16_t (&s)[KB], bool some, const uint32_t (&vis)[KB], int fk, float c2, float& m,
                                              float& l, f32x16_t (&o)[DB]) {
-  if (some) {
+  if (MASK == kDraft || some) {
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-      for (int e = 0; e < 16; ++e)
-        s[kb][e] = vis[kb] >> (4 * fk) >> (8 * (e >> 2) + (e & 3)) & 1 ? s[kb][e] : kLowest;
+      for (int e = 0; e < 16; ++e) s[kb][e] = tree_masked(s[kb][e], vis[kb] >> (4 * fk) >> (8 * (e >> 2) + (e & 3)) & 1);
   }
   float mx = kLowest;
 #pragma unroll
@@ -206,12 +261,15 @@ __device__ __forceinline__ void tree_softmax(f32x16_t (&s)[KB], bool some, const
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       float p = __builtin_amdgcn_exp2f(fmaf(s[kb][e], c2, -m));
-      if (some) p = vis[kb] >> (4 * fk) >> (8 * (e >> 2) + (e & 3)) & 1 ? p : 0.f;
+      if (MASK == kDraft) p = vis[kb] >> (4 * fk) >> (8 * (e >> 2) + (e & 3)) & 1 ? p : 0.f;
       s[kb][e] = p;
       sum += p;
     }
   l += sum;
 }
+// Scores to log2 units.  A negative scale is a positive one on queries of the other sign; 0 is taken as a
+// number that a masked score times it is still far below all others.
+__device__ __forceinline__ float tree_c2(float scale) { return fmaxf(fabsf(scale) * 1.4426950408889634f, 1e-30f); }
 
 // Four output values of a finished row.
 template <typename T16>
@@ -235,7 +293,7 @@ __device__ __forceinline__ float tree_inv(float l) { return l == 0.f ? 0.f : 1.0
 // ------------------------------------------------------------------------------------
 constexpr int TS_WAVES = 3;
 template <typename T16, int D, int QW, bool SMALL>
-__global__ __launch_bounds__(64 * TS_WAVES) void k_tree_stream(TreeArgs a, int shares, int least) {
+__device__ __forceinline__ void tree_stream(const TreeArgs& a, int shares, int least, int slack) {
 #if defined(__HIP_DEVICE_COMPILE__)
   typedef Half16<T16> H;
   typedef typename H::V8 V8;
@@ -250,11 +308,10 @@ __global__ __launch_bounds__(64 * TS_WAVES) void k_tree_stream(TreeArgs a, int s
   const int fr = lane & 31, fk = lane >> 5;
   const int g = blockIdx.x % a.Hkv, w = blockIdx.x / a.Hkv;
   const int G = a.Hq / a.Hkv;
-  int b, t0;
-  const TreeShares sh = tree_find<64 * NW, KT>(
-      a, shares, least, [&](const TreeShares& s) { return w < s.shares ? s.begin(w) : (int64_t)-1; }, &b, &t0);
-  if (sh.tiles == 0 || w >= sh.shares) return;
-  int64_t left = sh.begin(w + 1) - sh.begin(w);
+  TreePiece pc;
+  const TreeShares sh = tree_find<64 * NW, KT>(a, shares, least, slack, w, &pc);
+  int b = pc.b, t0 = pc.t;
+  int64_t left = pc.left;
 
   const uint32_t row_bytes = (uint32_t)a.Hkv * D * sizeof(T16);
   uint32_t koff[LOADS], voff[LOADS];
@@ -264,8 +321,7 @@ __global__ __launch_bounds__(64 * TS_WAVES) void k_tree_stream(TreeArgs a, int s
     koff[j] = (uint32_t)from * row_bytes + (uint32_t)((cp ^ kswz<D>(key)) * 16);
     voff[j] = (uint32_t)from * row_bytes + (uint32_t)((cp ^ vswz<D>(key)) * 16);
   }
-  // a negative scale is a positive one on queries of the other sign
-  const float c2 = fabsf(a.scale) * 1.4426950408889634f;
+  const float c2 = tree_c2(a.scale);
   const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
   const int tr_p = lane & 15;
   const int tr_key = fk * 4 + (tr_p >> 2);
@@ -276,6 +332,7 @@ __global__ __launch_bounds__(64 * TS_WAVES) void k_tree_stream(TreeArgs a, int s
     if (nn == 0) continue;
     const int P0 = (n0 + KT - 1) / KT, nt = P0 + (nn + KT - 1) / KT;
     const int t1 = __builtin_amdgcn_readfirstlane(t0 + (int)min((int64_t)(nt - t0), left)), rows = nn * G;
+    if (t0 == 0 && g == 0) tree_note(a, sh, b, w, sh.chunk ? 0 : sh.begin(w + 1) - left, nt);
     left -= t1 - t0;
     // This wave's tiles are t0 + wave + NW i.  Of drafted tokens there are two tiles at most (N <= 64),
     // next to each other, so a wave has one at most: td, which it takes first, where the one copy of
@@ -360,13 +417,12 @@ __global__ __launch_bounds__(64 * TS_WAVES) void k_tree_stream(TreeArgs a, int s
         // s[qi][0][e] = score(key 8(e/4) + 4 fk + e%4, row fr)
         const bool cached = !FIRST || i >= 0;
         const int there = n0 - (ts + NW * i) * KT;
-        const bool some = !cached || there < KT;
         const uint32_t tail = there >= KT ? ~0u : (1u << (there & 31)) - 1;
         const T16* vbase = reinterpret_cast<const T16*>(Vc);
 #pragma unroll
         for (int qi = 0; qi < QW; ++qi) {
           const uint32_t vis[1] = {cached ? tail : drafted[qi]};
-          tree_softmax<DB, 1>(s[qi], some, vis, fk, c2, m[qi], l[qi], o[qi]);
+          tree_softmax<DB, 1, FIRST ? kDraft : kTail>(s[qi], there < KT, vis, fk, c2, m[qi], l[qi], o[qi]);
         }
         if (!cached) {
           bool odd = false;
@@ -504,44 +560,59 @@ __global__ __launch_bounds__(64 * TS_WAVES) void k_tree_stream(TreeArgs a, int s
 #endif
 }
 
+// (One wave a SIMD could have 512 registers, but half of them only by way of moves: 32 rows stay in 256.)
+template <typename T16, int D, bool SMALL>
+__global__ __launch_bounds__(64 * TS_WAVES) __attribute__((amdgpu_num_vgpr(256))) void k_tree_stream32(TreeArgs a, int shares, int least, int slack) {
+  tree_stream<T16, D, 1, SMALL>(a, shares, least, slack);
+}
+template <typename T16, int D, bool SMALL>
+__global__ __launch_bounds__(64 * TS_WAVES) void k_tree_stream64(TreeArgs a, int shares, int least, int slack) {
+  tree_stream<T16, D, 2, SMALL>(a, shares, least, slack);
+}
+
 // ------------------------------------------------------------------------------------
-// More rows (large trees): bound by the matrix cores.  Blocks of NW x 32 rows share 64-key tiles, the
-// next tile's copies in flight under the present one, as in the prefix kernel.  The row blocks of one
-// share of tiles run next to each other on one XCD, so that its L2 serves all but the first.
+// More rows (large trees).  A workgroup's four waves hold 32 rows each and share tiles of 32 keys in a ring
+// of four stages; two workgroups share a CU.  One barrier a tile: behind it the tile has landed for every
+// wave and the one before has been read by all, so its stage takes the copies of the tile three further
+// on.
 // ------------------------------------------------------------------------------------
-template <typename T16, int D, int NW, bool SMALL>
-__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
-void k_tree_block(TreeArgs a, int shares, int least, int RB) {
+template <int N>
+__device__ __forceinline__ void tree_ring_step() {  // this wave's copies but the last N have landed; all waves are here
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+template <typename T16, int D>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void k_tree_block(TreeArgs a, int shares, int least, int slack, int RB) {
 #if defined(__HIP_DEVICE_COMPILE__)
   typedef Half16<T16> H;
   typedef typename H::V8 V8;
-  constexpr int BQ = NW * 32, KT = 64, CH = D / 8, KSTEPS = D / 16, DB = D / 32, KB = KT / 32;
+  constexpr int NW = 4, BQ = NW * 32, KT = 32, NS = 4, CH = D / 8, KSTEPS = D / 16, DB = D / 32;
   constexpr int LOADS = KT * CH / (NW * 64), KW = KT / NW;  // a wave copies KW keys of a tile
-  constexpr int NG = SMALL ? KW / 8 : 1, GL = LOADS / NG;
-  static_assert(KW % 8 == 0 && LOADS % NG == 0, "whole groups of 8 keys");
-  __shared__ u32x4_t Ks0[KT * CH], Ks1[KT * CH], Vs0[KT * CH], Vs1[KT * CH];
+  static_assert(KW <= 8 && LOADS * 64 == KW * CH, "a wave's keys lie in one page");
+  __shared__ u32x4_t S0[2 * KT * CH], S1[2 * KT * CH], S2[2 * KT * CH], S3[2 * KT * CH];  // K tile, V tile
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int fr = lane & 31, fk = lane >> 5;
   const int G = a.Hq / a.Hkv;
+  // the row blocks of one share next to each other on one XCD: its L2 serves all but the first
   const int local = blockIdx.x >> 3, pair = local / RB * 8 + (blockIdx.x & 7), rb = local % RB;
   const int g = pair % a.Hkv, w = pair / a.Hkv;
   if (w >= shares) return;
-  int b, t0;
-  const TreeShares sh = tree_find<64 * NW, KT>(
-      a, shares, least, [&](const TreeShares& s) { return w < s.shares ? s.begin(w) : (int64_t)-1; }, &b, &t0);
-  if (sh.tiles == 0 || w >= sh.shares) return;
-  int64_t left = sh.begin(w + 1) - sh.begin(w);
+  TreePiece pc;
+  const TreeShares sh = tree_find<64 * NW, KT>(a, shares, least, slack, w, &pc);
+  int b = pc.b, t0 = pc.t;
+  int64_t left = pc.left;
 
   const uint32_t row_bytes = (uint32_t)a.Hkv * D * sizeof(T16);
   uint32_t koff[LOADS], voff[LOADS];
 #pragma unroll
   for (int j = 0; j < LOADS; ++j) {
-    const int slot = (wave * LOADS + j) * 64 + lane, key = slot / CH, cp = slot % CH, from = (key - wave * KW) & (SMALL ? 7 : KW - 1);
+    const int slot = (wave * LOADS + j) * 64 + lane, key = slot / CH, cp = slot % CH, from = key - wave * KW;
     koff[j] = (uint32_t)from * row_bytes + (uint32_t)((cp ^ kswz<D>(key)) * 16);
     voff[j] = (uint32_t)from * row_bytes + (uint32_t)((cp ^ vswz<D>(key)) * 16);
   }
-  const float c2 = fabsf(a.scale) * 1.4426950408889634f;
+  const float c2 = tree_c2(a.scale);
   const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
   const int tr_p = lane & 15;
   const int tr_key = fk * 4 + (tr_p >> 2);
@@ -552,6 +623,7 @@ void k_tree_block(TreeArgs a, int shares, int least, int RB) {
     if (nn == 0) continue;
     const int P0 = (n0 + KT - 1) / KT, nt = P0 + (nn + KT - 1) / KT;
     const int t1 = __builtin_amdgcn_readfirstlane(t0 + (int)min((int64_t)(nt - t0), left)), rows = nn * G;
+    if (t0 == 0 && g == 0 && rb == 0) tree_note(a, sh, b, w, sh.chunk ? 0 : sh.begin(w + 1) - left, nt);
     left -= t1 - t0;
     if (rb * BQ >= rows) continue;
     const int64_t row0 = (int64_t)b * a.N;
@@ -569,128 +641,125 @@ void k_tree_block(TreeArgs a, int shares, int least, int RB) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[db][e] = 0.f;
 
-    // One tile from (Kc, Vc): cached tokens, `there` of them from its first on, or (DRAFT) drafted ones.
-    auto compute = [&](const u32x4_t* Kc, u32x4_t* Vc, int there, uint32_t d0, uint32_t d1, auto draft_) __attribute__((always_inline)) {
-      constexpr bool DRAFT = decltype(draft_)::value;
-      f32x16_t s[KB];
+    // s[e] = score(key 8(e/4) + 4 fk + e%4 of the tile in R, row fr)
+    auto scores = [&](const u32x4_t* R, f32x16_t& s) __attribute__((always_inline)) {
 #pragma unroll
-      for (int ks = 0; ks < KSTEPS; ++ks)
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
-          const int key = kb * 32 + fr;
-          const V8 kf = __builtin_bit_cast(V8, Kc[key * CH + ((ks * 2 + fk) ^ kswz<D>(key))]);
-          s[kb] = H::mma(kf, qf[ks], ks == 0 ? f32x16_t{} : s[kb]);
-        }
-      uint32_t vis[KB] = {d0, d1};
-      if (!DRAFT) {
-        vis[0] = there >= 32 ? ~0u : (1u << (there & 31)) - 1;
-        vis[1] = there >= 64 ? ~0u : there <= 32 ? 0u : (1u << (there & 31)) - 1;
+      for (int ks = 0; ks < KSTEPS; ++ks) {
+        const V8 kf = __builtin_bit_cast(V8, R[fr * CH + ((ks * 2 + fk) ^ kswz<D>(fr))]);
+        s = H::mma(kf, qf[ks], ks == 0 ? f32x16_t{} : s);
       }
-      tree_softmax<DB, KB>(s, DRAFT || there < KT, vis, fk, c2, m, l, o);
-      const T16* vbase = reinterpret_cast<const T16*>(Vc);
-      if (DRAFT) {  // (every wave looks at the whole tile, so that all of them agree)
-        bool odd = false;
-#pragma unroll
-        for (int j = 0; j < KT * CH / 64; ++j) {
-          const u32x4_t x = Vc[j * 64 + lane];
-          odd |= not_finite<T16>(x[0]) || not_finite<T16>(x[1]) || not_finite<T16>(x[2]) || not_finite<T16>(x[3]);
-        }
-        if (__any(odd)) {
-          tree_odd_values<T16, D>(vbase, 0, vis[0], fk, o);
-          tree_odd_values<T16, D>(vbase, 32, vis[1], fk, o);
-          __syncthreads();
-#pragma unroll
-          for (int j = 0; j < LOADS; ++j) Vc[(wave * LOADS + j) * 64 + lane] = tree_clean<T16>(Vc[(wave * LOADS + j) * 64 + lane]);
-          __syncthreads();
-        }
-      }
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int hh = 0; hh < 2; ++hh) {
-          const f32x16_t& x = s[kb];
-          const V8 pf = H::as_v8(make_uint4(H::pack2(x[hh * 8 + 0], x[hh * 8 + 1]), H::pack2(x[hh * 8 + 2], x[hh * 8 + 3]),
-                                            H::pack2(x[hh * 8 + 4], x[hh * 8 + 5]), H::pack2(x[hh * 8 + 6], x[hh * 8 + 7])));
-          const int ka = kb * 32 + hh * 16 + tr_key, kc = ka + 8;
-#pragma unroll
-          for (int db = 0; db < DB; ++db) {
-            const int col = db * 32 + tr_col;
-            const int ca = ((col >> 3) ^ vswz<D>(ka)) * 8 + (col & 7);
-            const int cc = ((col >> 3) ^ vswz<D>(kc)) * 8 + (col & 7);
-            const v4i16_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t*)(vbase + ka * D + ca));
-            const v4i16_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t*)(vbase + kc * D + cc));
-            const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
-            o[db] = H::mma(H::as_v8(make_uint4(l2.x, l2.y, h2.x, h2.y)), pf, o[db]);
-          }
-        }
     };
-    // Copies this wave's KW of the tokens from `first` on, of n (cached: in page pg[q] each 8 or all).
-    auto copy = [&](u32x4_t* Kd, u32x4_t* Vd, const void* kp, const void* vp, int first, int n, const int* pg) __attribute__((always_inline)) {
-      const char* kb = (const char*)kp + (int64_t)g * D * sizeof(T16);
-      const char* vb = (const char*)vp + (int64_t)g * D * sizeof(T16);
+    // o += V^T P^T of the tile in R
+    auto values = [&](const u32x4_t* R, const f32x16_t& x) __attribute__((always_inline)) {
+      const T16* vbase = reinterpret_cast<const T16*>(R + KT * CH);
 #pragma unroll
-      for (int q = 0; q < NG; ++q) {
-        const int from = first + wave * KW + 8 * q;
-        const int64_t row = pg ? ((int64_t)pg[q] << a.lg) + (from & ((1 << a.lg) - 1)) : row0 + from;
-        const int c = min(SMALL ? 8 : KW, n - from);
-        const int ext = c > 0 ? (int)((uint32_t)(c - 1) * row_bytes + D * (uint32_t)sizeof(T16)) : 0;
-        const __amdgpu_buffer_rsrc_t rk =
-            __builtin_amdgcn_make_buffer_rsrc(uniform_ptr((void*)(kb + row * row_bytes)), 0, __builtin_amdgcn_readfirstlane(ext), 0x00020000);
-        const __amdgpu_buffer_rsrc_t rv =
-            __builtin_amdgcn_make_buffer_rsrc(uniform_ptr((void*)(vb + row * row_bytes)), 0, __builtin_amdgcn_readfirstlane(ext), 0x00020000);
+      for (int hh = 0; hh < 2; ++hh) {
+        const V8 pf = H::as_v8(make_uint4(H::pack2(x[hh * 8 + 0], x[hh * 8 + 1]), H::pack2(x[hh * 8 + 2], x[hh * 8 + 3]),
+                                          H::pack2(x[hh * 8 + 4], x[hh * 8 + 5]), H::pack2(x[hh * 8 + 6], x[hh * 8 + 7])));
+        const int ka = hh * 16 + tr_key, kc = ka + 8;
 #pragma unroll
-        for (int j = q * GL; j < (q + 1) * GL; ++j) {
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void_t*)(Kd + (wave * LOADS + j) * 64), 16, koff[j], 0, 0, 0);
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void_t*)(Vd + (wave * LOADS + j) * 64), 16, voff[j], 0, 0, 0);
+        for (int db = 0; db < DB; ++db) {
+          const int col = db * 32 + tr_col;
+          const int ca = ((col >> 3) ^ vswz<D>(ka)) * 8 + (col & 7);
+          const int cc = ((col >> 3) ^ vswz<D>(kc)) * 8 + (col & 7);
+          const v4i16_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t*)(vbase + ka * D + ca));
+          const v4i16_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t*)(vbase + kc * D + cc));
+          const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
+          o[db] = H::mma(H::as_v8(make_uint4(l2.x, l2.y, h2.x, h2.y)), pf, o[db]);
         }
       }
     };
-    int pid[NG], seg = t0;  // page ids of this wave's tokens in tiles seg + lane
-    auto load_pages = [&](int first) {
-      seg = first;
+    // Drafted tile d from R, whole.
+    auto draft = [&](u32x4_t* R, int d) __attribute__((always_inline)) {
+      f32x16_t s[1];
+      scores(R, s[0]);
+      const uint32_t vis[1] = {tree_word(a, b, ri, d, nn)};
+      tree_softmax<DB, 1, kDraft>(s, true, vis, fk, c2, m, l, o);
+      u32x4_t* Vc = R + KT * CH;
+      bool odd = false;  // (every wave looks at the whole tile, so that all of them agree)
+#pragma unroll 2
+      for (int j = 0; j < KT * CH / 64; ++j) {
+        const u32x4_t x = Vc[j * 64 + lane];
+        odd |= not_finite<T16>(x[0]) || not_finite<T16>(x[1]) || not_finite<T16>(x[2]) || not_finite<T16>(x[3]);
+      }
+      if (__any(odd)) {
+        tree_odd_values<T16, D>(reinterpret_cast<const T16*>(Vc), 0, vis[0], fk, o);
+        __syncthreads();
 #pragma unroll
-      for (int q = 0; q < NG; ++q) {
-        const int token = min((seg + lane) * KT + wave * KW + 8 * q, n0 - 1);
-        pid[q] = seg + lane < min(t1, P0) && token >= 0 ? tree_page(a, b, token) : 0;
+        for (int j = 0; j < LOADS; ++j) Vc[(wave * LOADS + j) * 64 + lane] = tree_clean<T16>(Vc[(wave * LOADS + j) * 64 + lane]);
+        __syncthreads();
+      }
+      values(R, s[0]);
+    };
+    // Copies this wave's KW of the tokens from `first` on, of n (cached: in page `page`).
+    auto copy = [&](u32x4_t* R, bool cached, int first, int n, int page) __attribute__((always_inline)) {
+      const int from = first + wave * KW, c = min(KW, n - from);
+      const int64_t row = cached ? ((int64_t)page << a.lg) + (from & ((1 << a.lg) - 1)) : row0 + from;
+      const int64_t at = row * row_bytes + (int64_t)g * D * sizeof(T16);
+      const int ext = c > 0 ? (int)((uint32_t)(c - 1) * row_bytes + D * (uint32_t)sizeof(T16)) : 0;
+      const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(
+          uniform_ptr((void*)((const char*)(cached ? a.k : a.kn) + at)), 0, __builtin_amdgcn_readfirstlane(ext), 0x00020000);
+      const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(
+          uniform_ptr((void*)((const char*)(cached ? a.v : a.vn) + at)), 0, __builtin_amdgcn_readfirstlane(ext), 0x00020000);
+#pragma unroll
+      for (int j = 0; j < LOADS; ++j) {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void_t*)(R + (wave * LOADS + j) * 64), 16, koff[j], 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void_t*)(R + KT * CH + (wave * LOADS + j) * 64), 16, voff[j], 0, 0, 0);
       }
     };
-    auto load = [&](u32x4_t* Kd, u32x4_t* Vd, int t) __attribute__((always_inline)) {
-      int pg[NG];
-#pragma unroll
-      for (int q = 0; q < NG; ++q) pg[q] = __builtin_amdgcn_readlane(pid[q], t - seg);
-      copy(Kd, Vd, a.k, a.v, t * KT, n0, pg);
-    };
-    // Drafted tiles first (in buffer 0), in the one copy of the code for masks and odd values; the cached
-    // ones then start from buffer 1.
+    // Cached tiles in segments of 128, whose page ids a wave holds two a lane.  Tile k of a segment is in
+    // stage (k + 1) % NS.  Drafted tiles come first, in stage 0, with the first cached ones on their way.
     const int te = min(t1, P0);
-    if (t0 < te) load_pages(t0);
-    for (int t = max(t0, P0); t < t1; ++t) {
-      const int d = t - P0;
-      const uint32_t d0 = tree_word(a, b, ri, 2 * d, nn), d1 = 2 * d + 1 < a.W ? tree_word(a, b, ri, 2 * d + 1, nn) : 0u;
-      copy(Ks0, Vs0, a.kn, a.vn, d * KT, nn, nullptr);
-      if (t + 1 == t1 && t0 < te) load(Ks1, Vs1, t0);
-      __syncthreads();
-      compute(Ks0, Vs0, 0, d0, d1, std::true_type{});
-      __syncthreads();
-    }
-    for (int from = t0; from < te; from += 64) {
-      const int se = min(te, from + 64);
-      if (from > t0) load_pages(from);
-      if (from > t0 || t1 <= P0) {
-        load(Ks1, Vs1, from);
-        __syncthreads();
+    int drafts = t1 - max(t0, P0);
+    for (int from = t0; from < te || drafts > 0; from += 128) {
+      const int n = min(te - from, 128);
+      int pid[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int token = min((from + 64 * h + lane) * KT + wave * KW, n0 - 1);
+        pid[h] = 64 * h + lane < n && token >= 0 ? tree_page(a, b, token) : 0;
       }
-      auto tile = [&](const u32x4_t* Kc, u32x4_t* Vc, u32x4_t* Kn, u32x4_t* Vn, int t) __attribute__((always_inline)) {
-        if (t + 1 < se) load(Kn, Vn, t + 1);
-        compute(Kc, Vc, n0 - t * KT, 0u, 0u, std::false_type{});
-        __syncthreads();
+      auto load = [&](u32x4_t* R, int k) __attribute__((always_inline)) {  // (past the segment: nothing is fetched)
+        const int p0 = __builtin_amdgcn_readlane(pid[0], k & 63), p1 = __builtin_amdgcn_readlane(pid[1], k & 63);
+        copy(R, true, (from + k) * KT, k < n ? n0 : 0, k < 64 ? p0 : p1);
       };
-      int t = from;
-      for (; t + 2 <= se; t += 2) {
-        tile(Ks1, Vs1, Ks0, Vs0, t);
-        tile(Ks0, Vs0, Ks1, Vs1, t + 1);
+      __syncthreads();  // the stages are free
+      if (drafts > 0) copy(S0, false, (max(t0, P0) - P0) * KT, nn, 0);
+      load(S1, 0);
+      load(S2, 1);
+      load(S3, 2);
+      if (drafts > 0) {
+        tree_ring_step<(NS - 1) * 2 * LOADS>();
+        int d = max(t0, P0) - P0;
+        for (;;) {
+          draft(S0, d);
+          if (--drafts <= 0) break;
+          ++d;
+          __syncthreads();
+          copy(S0, false, d * KT, nn, 0);
+          __syncthreads();
+        }
       }
-      if (t < se) tile(Ks1, Vs1, Ks0, Vs0, t);
+      // Tile k.  The copies are issued past the last tile too, so that the compiler counts them exactly.
+      auto step = [&](u32x4_t* next, const u32x4_t* now, int k) __attribute__((always_inline)) {
+        tree_ring_step<(NS - 2) * 2 * LOADS>();
+        load(next, k + NS - 1);
+        if (k < n) {
+          f32x16_t s[1];
+          scores(now, s[0]);
+          const int there = n0 - (from + k) * KT;
+          const uint32_t vis[1] = {(1u << (there & 31)) - 1};  // (where the tile is not full)
+          tree_softmax<DB, 1, kTail>(s, there < KT, vis, fk, c2, m, l, o);
+          values(now, s[0]);
+        }
+      };
+      for (int k = 0; k < n; k += NS) {
+        step(S0, S1, k);
+        step(S1, S2, k + 1);
+        step(S2, S3, k + 2);
+        step(S3, S0, k + 3);
+      }
+      __builtin_amdgcn_s_waitcnt(0);
     }
 
     // o[db][e] = O^T(dim db*32 + 8(e/4) + 4 fk + e%4, row r)
@@ -723,7 +792,7 @@ void k_tree_block(TreeArgs a, int shares, int least, int RB) {
 // kernel, and join their sums in LDS.
 // ------------------------------------------------------------------------------------
 template <int D, int NW>
-__global__ __launch_bounds__(NW * 64) void k_tree_f32(TreeArgs a, int shares, int least, int RB) {
+__global__ __launch_bounds__(NW * 64) void k_tree_f32(TreeArgs a, int shares, int least, int slack, int RB) {
   constexpr int KT = 32, NC = D / 8, DB = D / 32;
   __shared__ float4 part[NW][DB * 4][64];
   __shared__ float2 ml[NW][64];
@@ -732,11 +801,10 @@ __global__ __launch_bounds__(NW * 64) void k_tree_f32(TreeArgs a, int shares, in
   const int fr = lane & 31, fk = lane >> 5;
   const int G = a.Hq / a.Hkv;
   const int rb = blockIdx.x % RB, g = blockIdx.x / RB % a.Hkv, w = blockIdx.x / RB / a.Hkv;
-  int b, t0;
-  const TreeShares sh = tree_find<64 * NW, KT>(
-      a, shares, least, [&](const TreeShares& s) { return w < s.shares ? s.begin(w) : (int64_t)-1; }, &b, &t0);
-  if (sh.tiles == 0 || w >= sh.shares) return;
-  int64_t left = sh.begin(w + 1) - sh.begin(w);
+  TreePiece pc;
+  const TreeShares sh = tree_find<64 * NW, KT>(a, shares, least, slack, w, &pc);
+  int b = pc.b, t0 = pc.t;
+  int64_t left = pc.left;
   const int64_t ld = (int64_t)a.Hkv * D;
 
   for (; left > 0; ++b, t0 = 0) {
@@ -744,6 +812,7 @@ __global__ __launch_bounds__(NW * 64) void k_tree_f32(TreeArgs a, int shares, in
     if (nn == 0) continue;
     const int P0 = (n0 + KT - 1) / KT, nt = P0 + (nn + KT - 1) / KT;
     const int t1 = __builtin_amdgcn_readfirstlane(t0 + (int)min((int64_t)(nt - t0), left)), rows = nn * G;
+    if (t0 == 0 && g == 0 && rb == 0) tree_note(a, sh, b, w, sh.chunk ? 0 : sh.begin(w + 1) - left, nt);
     left -= t1 - t0;
     if (rb * 32 >= rows) continue;
     const int64_t row0 = (int64_t)b * a.N;
@@ -908,79 +977,128 @@ __global__ __launch_bounds__(NW * 64) void k_tree_f32(TreeArgs a, int shares, in
   }
 }
 
-// Joins the records of the sequences that several shares hold, one wave a row, shares in order; zeroes
-// the padding rows where asked.  One workgroup per (sequence, kv head, TM_ROWS rows).
-constexpr int TM_ROWS = 16;
-template <typename T, int D, int KT>
-__global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a, int most, int least, int BQ, int RB) {
-  constexpr int PER = D / 64;
-  const int lane = threadIdx.x & 63;
+// ------------------------------------------------------------------------------------
+// Joins the records of the sequences that several shares hold; zeroes the padding rows where asked.
+// Bound by latency (which shares, their maxima and sums, their o: three loads in a row), so a wave has
+// many of each in flight.  Few rows (one sequence in many shares): a wave a row, its halves taking
+// every other record.  Many rows (few shares each): eight rows a wave, a lane for each of their
+// maxima, each half taking every other row.
+// ------------------------------------------------------------------------------------
+constexpr int TM_WAVES = 4, TM_MANY = 8;
+template <typename T, int D, int ROWS>
+__global__ __launch_bounds__(64 * TM_WAVES) void k_tree_merge(TreeArgs a, int BQ, int RB) {
+  constexpr int PER = D / 32;
+  typedef float vec_t __attribute__((ext_vector_type(PER)));
+  const int lane = threadIdx.x & 63, half = lane >> 5, at = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int groups = (a.N * (a.Hq / a.Hkv) + TM_ROWS - 1) / TM_ROWS;
-  const int r0 = blockIdx.x % groups * TM_ROWS, g = blockIdx.x / groups % a.Hkv, b = blockIdx.x / groups / a.Hkv;
-  const int G = a.Hq / a.Hkv, nn = tree_nodes(a, b), rows = nn * G;
-  const int64_t row0 = (int64_t)b * a.N;
+  const int G = a.Hq / a.Hkv, groups = (a.N * G + TM_WAVES * ROWS - 1) / (TM_WAVES * ROWS);
+  const int r0 = (blockIdx.x % groups * TM_WAVES + wave) * ROWS, g = blockIdx.x / groups % a.Hkv, b = blockIdx.x / groups / a.Hkv;
+  const int rows = tree_nodes(a, b) * G;
+  auto out_at = [&](int r) {
+    const int i = r / G;
+    return (T*)a.out + (((int64_t)b * a.N + i) * a.Hq + g * G + r - i * G) * D + at * PER;
+  };
   if (a.zero_rest) {
-    for (int r = max(r0, rows) + wave; r < min(r0 + TM_ROWS, a.N * G); r += 4) {
-      const int i = r / G;
-      T* op = (T*)a.out + ((row0 + i) * a.Hq + g * G + r - i * G) * D + lane * PER;
+    for (int r = max(r0, rows) + half; r < min(r0 + ROWS, a.N * G); r += 2) {
 #pragma unroll
-      for (int c = 0; c < PER; ++c) stf(op + c, 0.f);
+      for (int c = 0; c < PER; ++c) stf(out_at(r) + c, 0.f);
     }
   }
   if (r0 >= rows) return;
-  // tiles before this sequence, and of all
-  __shared__ int64_t red[8];
-  int64_t before = 0, all = 0;
-  for (int x = threadIdx.x; x < a.B; x += 256) {
-    const int n = tree_tiles<KT>(a, x);
-    all += n;
-    before += x < b ? n : 0;
-  }
-  before = wave_sum((long long)before);
-  all = wave_sum((long long)all);
-  if (lane == 0) {
-    red[wave] = before;
-    red[4 + wave] = all;
-  }
-  __syncthreads();
-  before = red[0] + red[1] + red[2] + red[3];
-  TreeShares sh;
-  sh.tiles = red[4] + red[5] + red[6] + red[7];
-  const int64_t fit = sh.tiles / least;
-  sh.shares = fit < 1 ? 1 : fit < most ? (int)fit : most;
-  const int wa = __builtin_amdgcn_readfirstlane(sh.owner(before));
-  const int wb = __builtin_amdgcn_readfirstlane(sh.owner(before + tree_tiles<KT>(a, b) - 1));
+  const int2 held = a.held[b];
+  const int wa = __builtin_amdgcn_readfirstlane(held.x), wb = __builtin_amdgcn_readfirstlane(held.y);
   if (wa == wb) return;  // one share held it all
-  for (int r = r0 + wave; r < min(r0 + TM_ROWS, rows); r += 4) {
-    const int rb = r / BQ, in = r - rb * BQ;
-    auto record = [&](int w) { return a.part + tree_record_at(a, w, w == wa, g, rb, RB, BQ); };
-    float M = kLowest;
-    for (int w = wa + lane; w <= wb; w += 64) M = fmaxf(M, record(w)[BQ * D + 2 * in]);
-    M = wave_max(M);
-    float L = 0.f, o[PER] = {};
+  auto record = [&](int w, int rb) { return a.part + tree_record_at(a, w, w == wa, g, rb, RB, BQ); };
+  if constexpr (ROWS == 1) {
+    const int rb = r0 / BQ, in = r0 - rb * BQ;
+    float M = kLowest, L = 0.f;
+    vec_t o = {};
     for (int base = wa; base <= wb; base += 64) {
-      const int w = base + lane;
-      float f = 0.f;
-      if (w <= wb) {
-        const float2 x = *reinterpret_cast<const float2*>(record(w) + BQ * D + 2 * in);
-        f = __builtin_amdgcn_exp2f(x.x - M);
-        L = fmaf(x.y, f, L);
-      }
+      float2 x = make_float2(kLowest, 0.f);
+      if (base + lane <= wb) x = *reinterpret_cast<const float2*>(record(base + lane, rb) + BQ * D + 2 * in);
+      const float mn = fmaxf(M, wave_max(x.x)), old = __builtin_amdgcn_exp2f(M - mn);
+      const float f = __builtin_amdgcn_exp2f(x.x - mn);
+      M = mn;
+      L = fmaf(x.y, f, L * old);
+      o *= old;
       const int n = min(64, wb - base + 1);
-#pragma unroll 4
-      for (int k = 0; k < n; ++k) {
-        const float z = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), k));
-        const float* x = record(base + k) + in * D + lane * PER;
+      for (int k = 0; k < n; k += 16) {
+        vec_t v[8];
 #pragma unroll
-        for (int c = 0; c < PER; ++c) o[c] = fmaf(x[c], z, o[c]);
+        for (int j = 0; j < 8; ++j) {  // (past the last: once more the last, with weight 0)
+          const int e = min(k + 2 * j + half, n - 1);
+          v[j] = *reinterpret_cast<const vec_t*>(record(base + e, rb) + in * D + at * PER);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int e = k + 2 * j + half;
+          const float z = __shfl(f, min(e, 63), kWave);
+          o += v[j] * (e < n ? z : 0.f);
+        }
       }
     }
     const float inv = tree_inv(wave_sum(L));
-    const int i = r / G;
-    T* op = (T*)a.out + ((row0 + i) * a.Hq + g * G + r - i * G) * D + lane * PER;
 #pragma unroll
-    for (int c = 0; c < PER; ++c) stf(op + c, o[c] * inv);
+    for (int c = 0; c < PER; ++c) {
+      const float y = (o[c] + __shfl_xor(o[c], 32, kWave)) * inv;
+      if (half == 0) stf(out_at(r0) + c, y);
+    }
+  } else {
+    static_assert(ROWS == 8, "eight rows by eight records a lane each");
+    // lane (j, e) holds the maximum and sum of row r0 + j in record e of eight
+    const int j8 = lane >> 3, e8 = lane & 7;
+    const int rj = min(r0 + j8, rows - 1), rbj = rj / BQ, inj = rj - rbj * BQ;
+    float M = kLowest, L = 0.f;
+    vec_t o[ROWS / 2] = {};
+    for (int base = wa; base <= wb; base += 8) {
+      float2 x = make_float2(kLowest, 0.f);
+      if (base + e8 <= wb) x = *reinterpret_cast<const float2*>(record(base + e8, rbj) + BQ * D + 2 * inj);
+      float mn = x.x;
+#pragma unroll
+      for (int s = 1; s < 8; s <<= 1) mn = fmaxf(mn, __shfl_xor(mn, s, kWave));
+      mn = fmaxf(M, mn);
+      const float old = __builtin_amdgcn_exp2f(M - mn), f = __builtin_amdgcn_exp2f(x.x - mn);
+      M = mn;
+      L = fmaf(x.y, f, L * old);
+      const int n = min(8, wb - base + 1);
+#pragma unroll
+      for (int p = 0; p < ROWS / 2; ++p) o[p] *= __shfl(old, (2 * p + half) * 8, kWave);
+      for (int e = 0; e < n; e += 2) {
+        vec_t v[2][ROWS / 2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int p = 0; p < ROWS / 2; ++p) {  // (past the last: once more the last, with weight 0)
+            const int r = min(r0 + 2 * p + half, rows - 1), rb = r / BQ;
+            v[u][p] = *reinterpret_cast<const vec_t*>(record(base + min(e + u, n - 1), rb) + (r - rb * BQ) * D + at * PER);
+          }
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int p = 0; p < ROWS / 2; ++p) {
+            const float z = __shfl(f, (2 * p + half) * 8 + ((e + u) & 7), kWave);
+            o[p] += v[u][p] * (e + u < n ? z : 0.f);
+          }
+      }
+    }
+#pragma unroll
+    for (int s = 1; s < 8; s <<= 1) L += __shfl_xor(L, s, kWave);
+    const float inv = tree_inv(L);
+#pragma unroll
+    for (int p = 0; p < ROWS / 2; ++p) {
+      const float z = __shfl(inv, (2 * p + half) * 8, kWave);
+      const int r = r0 + 2 * p + half;
+      if (r < rows) {
+        T* op = out_at(r);
+        if constexpr (PER == 4) {
+          const float y[4] = {o[p][0] * z, o[p][1] * z, o[p][2] * z, o[p][3] * z};
+          store4(op, y);
+        } else {
+#pragma unroll
+          for (int c = 0; c < PER; ++c) stf(op + c, o[p][c] * z);
+        }
+      }
+    }
   }
 }
 
@@ -1014,43 +1132,60 @@ __global__ __launch_bounds__(kMaxNodes) void k_tree_plan(int N, int W, const int
   positions[2 * rows + row] = pos;
 }
 
-// How a launch runs: rows of a block, row blocks, shares of the tiles (a share: one workgroup per kv head
-// and row block) and the least tiles of one.
+// How a launch runs: rows of a block (QW groups of 32 a wave), row blocks, shares of the tiles (a share:
+// one workgroup per kv head and row block), the least tiles of one, and how much longer chunks may be.
 struct TreePlan {
   bool stream;
-  int BQ, RB, shares, least;
+  int QW, BQ, RB, shares, least, slack;
 };
 static TreePlan tree_plan(rp_dtype dt, int32_t N, int32_t Hq, int32_t Hkv) {
   TreePlan p;
   const int rows = N * (Hq / Hkv);
   p.stream = dt != RP_F32 && rows <= 64;
-  p.BQ = dt == RP_F32 ? 32 : p.stream ? (rows <= 32 ? 32 : 64) : 128;
+  p.QW = p.stream ? (rows + 31) / 32 : 1;
+  p.BQ = dt == RP_F32 ? 32 : p.stream ? 32 * p.QW : 128;
   p.RB = (rows + p.BQ - 1) / p.BQ;
   // a stream workgroup has a CU's LDS to itself, of the others two share one
   p.shares = (p.stream ? 256 : 512) / (Hkv * p.RB);
   if (p.shares < 1) p.shares = 1;
   p.least = p.stream ? 3 : 4;
+  p.slack = p.stream ? 24 : 8;
   return p;
 }
 
-size_t tree_partial_floats(rp_dtype dt, int32_t, int32_t N, int32_t Hq, int32_t Hkv, int32_t D) {
-  const TreePlan p = tree_plan(dt, N, Hq, Hkv);
+static size_t tree_records(const TreePlan& p, int32_t Hkv, int32_t D) {
   return (size_t)p.shares * 2 * Hkv * p.RB * tree_record(p.BQ, D);
 }
+size_t tree_partial_floats(rp_dtype dt, int32_t B, int32_t N, int32_t Hq, int32_t Hkv, int32_t D) {
+  return tree_records(tree_plan(dt, N, Hq, Hkv), Hkv, D) + 2 * (size_t)B;
+}
 
-hipError_t launch_tree_attention(hipStream_t s, rp_dtype dt, const TreeArgs& a) {
+hipError_t launch_tree_attention(hipStream_t s, rp_dtype dt, const TreeArgs& args) {
+  TreeArgs a = args;
+  a.few = a.B <= 64 && (int64_t)a.B * (((int64_t)a.table_ld << a.lg) / 32 + kMaxNodes) < (int64_t)1 << 31;
   const TreePlan p = tree_plan(dt, a.N, a.Hq, a.Hkv);
+  a.held = reinterpret_cast<int2*>(a.part + tree_records(p, a.Hkv, a.D));
   typedef std::integral_constant<int, 128> D128;
   typedef std::integral_constant<int, 64> D64;
-  const int merge = (a.N * (a.Hq / a.Hkv) + TM_ROWS - 1) / TM_ROWS * a.Hkv * a.B;
+  // up to four rows a wave slot of the chip: a wave a row
+  const int rows = a.N * (a.Hq / a.Hkv), per = (int64_t)rows * a.Hkv * a.B <= 4096 ? 1 : TM_MANY;
+  const int64_t merge = (int64_t)((rows + TM_WAVES * per - 1) / (TM_WAVES * per)) * a.Hkv * a.B;
+  auto join = [&](auto t_, auto d_) {
+    typedef decltype(t_) T;
+    constexpr int D = decltype(d_)::value;
+    if (per == 1)
+      k_tree_merge<T, D, 1><<<merge, 64 * TM_WAVES, 0, s>>>(a, p.BQ, p.RB);
+    else
+      k_tree_merge<T, D, TM_MANY><<<merge, 64 * TM_WAVES, 0, s>>>(a, p.BQ, p.RB);
+  };
   if (dt == RP_F32) {
     const int grid = p.shares * a.Hkv * p.RB;
     if (a.D == 128) {
-      k_tree_f32<128, 4><<<grid, 256, 0, s>>>(a, p.shares, p.least, p.RB);
-      k_tree_merge<float, 128, 32><<<merge, 256, 0, s>>>(a, p.shares, p.least, p.BQ, p.RB);
+      k_tree_f32<128, 4><<<grid, 256, 0, s>>>(a, p.shares, p.least, p.slack, p.RB);
+      join(float(), D128{});
     } else {
-      k_tree_f32<64, 8><<<grid, 512, 0, s>>>(a, p.shares, p.least, p.RB);
-      k_tree_merge<float, 64, 32><<<merge, 256, 0, s>>>(a, p.shares, p.least, p.BQ, p.RB);
+      k_tree_f32<64, 8><<<grid, 512, 0, s>>>(a, p.shares, p.least, p.slack, p.RB);
+      join(float(), D64{});
     }
     return hipGetLastError();
   }
@@ -1061,20 +1196,17 @@ hipError_t launch_tree_attention(hipStream_t s, rp_dtype dt, const TreeArgs& a) 
       if (p.stream) {
         const int grid = p.shares * a.Hkv;
         const bool small = a.lg < 5;
-        if (p.BQ == 32)
-          small ? k_tree_stream<T, D, 1, true><<<grid, 64 * TS_WAVES, 0, s>>>(a, p.shares, p.least)
-                : k_tree_stream<T, D, 1, false><<<grid, 64 * TS_WAVES, 0, s>>>(a, p.shares, p.least);
+        if (p.QW == 1)
+          small ? k_tree_stream32<T, D, true><<<grid, 64 * TS_WAVES, 0, s>>>(a, p.shares, p.least, p.slack)
+                : k_tree_stream32<T, D, false><<<grid, 64 * TS_WAVES, 0, s>>>(a, p.shares, p.least, p.slack);
         else
-          small ? k_tree_stream<T, D, 2, true><<<grid, 64 * TS_WAVES, 0, s>>>(a, p.shares, p.least)
-                : k_tree_stream<T, D, 2, false><<<grid, 64 * TS_WAVES, 0, s>>>(a, p.shares, p.least);
-        k_tree_merge<T, D, 32><<<merge, 256, 0, s>>>(a, p.shares, p.least, p.BQ, p.RB);
+          small ? k_tree_stream64<T, D, true><<<grid, 64 * TS_WAVES, 0, s>>>(a, p.shares, p.least, p.slack)
+                : k_tree_stream64<T, D, false><<<grid, 64 * TS_WAVES, 0, s>>>(a, p.shares, p.least, p.slack);
+        join(T(), d_);
       } else {
         const int grid = (p.shares * a.Hkv + 7) / 8 * 8 * p.RB;
-        if (a.lg < 4)
-          k_tree_block<T, D, 4, true><<<grid, 256, 0, s>>>(a, p.shares, p.least, p.RB);
-        else
-          k_tree_block<T, D, 4, false><<<grid, 256, 0, s>>>(a, p.shares, p.least, p.RB);
-        k_tree_merge<T, D, 64><<<merge, 256, 0, s>>>(a, p.shares, p.least, p.BQ, p.RB);
+        k_tree_block<T, D><<<grid, 256, 0, s>>>(a, p.shares, p.least, p.slack, p.RB);
+        join(T(), d_);
       }
     };
     if (a.D == 128)

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from array import array
 from ctypes import POINTER, Structure, byref, c_char_p, c_double, c_float, c_int, c_int32, c_int64, \
     c_size_t, c_uint32, c_void_p
 from typing import Optional, Sequence
@@ -174,8 +175,12 @@ def _ptr(x) -> Optional[int]:
 def _i32(seq: Optional[Sequence[int]]):
     if seq is None:
         return None
-    vals = [int(v) for v in seq]
-    return (c_int32 * len(vals))(*vals)
+    try:
+        vals = array("i", seq)
+    except (TypeError, OverflowError):  # not a sequence of whole numbers that fit
+        vals = [int(v) for v in seq]
+        return (c_int32 * len(vals))(*vals)
+    return (c_int32 * len(vals)).from_buffer(vals) if vals else (c_int32 * 0)()
 
 
 def make_config(model, max_position: int, weight_layout: int = 0) -> RpConfig:

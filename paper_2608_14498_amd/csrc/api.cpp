@@ -1586,8 +1586,9 @@ rp_status rp_tree_commit(const rp_pages* pages, void* stream, int32_t B, int32_t
   if ((st = check_rows(*pages, draft, (int64_t)B * N, "draft")) != RP_OK) return st;
   hipStream_t s = (hipStream_t)stream;
   const rp::PageArgs a = page_args(*pages);
-  RP_TRY_LAUNCH_N("tree.walk", rp::launch_tree_walk(s, B, N, n_nodes, token_ids, parents, next_ids, accepted, n_accepted, token_out));
-  RP_TRY_LAUNCH_N("tree.commit_plan", rp::launch_commit_plan(s, a, B, N, accepted, n_accepted, token_out, missing));
+  const rp::TreePick t = {n_nodes, token_ids, parents, next_ids, accepted, n_accepted, token_out, N};
+  if (!rp::commit_walks(B, N)) RP_TRY_LAUNCH_N("tree.walk", rp::launch_tree_walk(s, t, B));
+  RP_TRY_LAUNCH_N("tree.commit_plan", rp::launch_commit_plan(s, a, t, B, missing));
   RP_TRY_LAUNCH_N("tree.commit_rows", rp::launch_commit_rows(s, a, B, N, accepted, n_accepted, draft.k, draft.v,
                                                              draft.layer_stride * pages_elem(*pages)));
   return RP_OK;

@@ -188,8 +188,7 @@ __global__ __launch_bounds__(256) void k_pages_free(PageArgs a, SeqRows q) {
   if (i < q.n) release(a, q.seq[i], threadIdx.x & 63);
 }
 
-// dst[i] gives its pages back, then shares the full pages of src[i] and gets a page of its own for
-// the rest.
+// dst[i] gives its pages back and gets one of its own for src[i]'s last page, where that is not full.
 __global__ __launch_bounds__(kPlanThreads) void k_fork_plan(PageArgs a, SeqPairs q, int32_t* __restrict__ missing) {
   __shared__ PlanShared sh;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
@@ -199,25 +198,26 @@ __global__ __launch_bounds__(kPlanThreads) void k_fork_plan(PageArgs a, SeqPairs
   const int in_page = (1 << a.lg) - 1;
   take_pages(a, q.n, sh, missing, [&](int i) { return (seq_len(a, q.src[i]) & in_page) ? 1 : 0; },
              [&](int i, int, int id) { a.table[(int64_t)q.dst[i] * a.table_ld + (seq_len(a, q.src[i]) >> a.lg)] = id; });
-  for (int i = w; i < q.n; i += kPlanWaves) {
-    if (missing[i] != 0) continue;
-    const int n = seq_len(a, q.src[i]);
+  for (int i = threadIdx.x; i < q.n; i += kPlanThreads)
+    if (missing[i] == 0) a.len[q.dst[i]] = seq_len(a, q.src[i]);
+}
+
+// The rest of a fork, one workgroup a pair, layer and matrix: the rows of src[i]'s last page, where it is not
+// full; the first one also shares the full pages.
+__global__ __launch_bounds__(256) void k_fork_rows(PageArgs a, SeqPairs q, const int32_t* __restrict__ missing) {
+  const int i = blockIdx.x;
+  if (missing[i] != 0) return;
+  const int n = seq_len(a, q.src[i]), rest = n & ((1 << a.lg) - 1);
+  if (blockIdx.y == 0 && blockIdx.z == 0) {
     const int32_t* from = a.table + (int64_t)q.src[i] * a.table_ld;
     int32_t* to = a.table + (int64_t)q.dst[i] * a.table_ld;
-    for (int j = lane; j < n >> a.lg; j += 64) {
+    for (int j = threadIdx.x; j < n >> a.lg; j += 256) {
       const int id = from[j];
       if (id >= 0 && id < a.n_pages) atomicAdd(a.refs + id, 1);
       to[j] = id;
     }
-    if (lane == 0) a.len[q.dst[i]] = n;
   }
-}
-
-// The rows of src[i]'s last page, where it is not full.
-__global__ __launch_bounds__(256) void k_fork_rows(PageArgs a, SeqPairs q, const int32_t* __restrict__ missing) {
-  const int i = blockIdx.x;
-  const int n = seq_len(a, q.src[i]), rest = n & ((1 << a.lg) - 1);
-  if (missing[i] != 0 || rest == 0) return;
+  if (rest == 0) return;
   const int64_t from = slot_of(a, q.src[i], n - rest), to = slot_of(a, q.dst[i], n - rest);
   if (from < 0 || to < 0) return;
   uint8_t* base = (blockIdx.z ? a.v : a.k) + blockIdx.y * a.layer_bytes;
@@ -230,27 +230,46 @@ __global__ __launch_bounds__(256) void k_fork_rows(PageArgs a, SeqPairs q, const
 // ascending order.  ws: [0] = moves, then map[n_pages] (new id of every page), from[], to[].
 __global__ __launch_bounds__(kPlanThreads) void k_compact_plan(PageArgs a, int32_t* __restrict__ n_live, int32_t* __restrict__ ws) {
   __shared__ int32_t wave[kPlanWaves];
-  int live = 0;
-  for (int base = 0; base < a.n_pages; base += kPlanThreads) {
-    const int id = base + (int)threadIdx.x;
-    int sum;
-    block_scan(id < a.n_pages && a.refs[id] > 0 ? 1 : 0, wave, &sum);
+  constexpr int kRound = 4 * kPlanThreads;
+  // bits 0..3: which of this thread's four pages of a round are in use; the first round's are kept
+  auto in_use = [&](int base) {
+    int bits = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int id = base + 4 * (int)threadIdx.x + i;
+      bits |= (id < a.n_pages && a.refs[id] > 0) << i;
+    }
+    return bits;
+  };
+  const int first = in_use(0);
+  int live = 0, sum;
+  for (int base = 0; base < a.n_pages; base += kRound) {
+    block_scan(__builtin_popcount(base ? in_use(base) : first), wave, &sum);
     live += sum;
   }
   int32_t *map = ws + 1, *from = map + a.n_pages, *to = from + a.n_pages / 2;
   int holes = 0, movers = 0;
-  for (int base = 0; base < a.n_pages; base += kPlanThreads) {
-    const int id = base + (int)threadIdx.x;
-    const bool in = id < a.n_pages, used = in && a.refs[id] > 0;
-    const int hole = in && !used && id < live, mover = used && id >= live;
-    int nh, nm;
-    const int rh = holes + block_scan(hole, wave, &nh) - 1;
-    const int rm = movers + block_scan(mover, wave, &nm) - 1;
-    if (hole) to[rh] = id;
-    if (mover) from[rm] = id;
-    if (in) map[id] = id;
-    holes += nh;
-    movers += nm;
+  for (int base = 0; base < a.n_pages; base += kRound) {
+    const int bits = base ? in_use(base) : first, id0 = base + 4 * (int)threadIdx.x;
+    int mine = 0;  // holes, and movers in the upper half (a round has 4096 of both together)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int id = id0 + i;
+      if (id < a.n_pages) mine += id < live ? !(bits >> i & 1) : (bits >> i & 1) << 16;
+    }
+    const int before = block_scan(mine, wave, &sum) - mine;
+    int h = holes + (before & 0xffff), m = movers + (before >> 16);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int id = id0 + i;
+      if (id >= a.n_pages) continue;
+      const bool used = bits >> i & 1;
+      map[id] = id;
+      if (id < live && !used) to[h++] = id;
+      if (id >= live && used) from[m++] = id;
+    }
+    holes += sum & 0xffff;
+    movers += sum >> 16;
   }
   __threadfence();
   __syncthreads();
@@ -292,53 +311,54 @@ __global__ __launch_bounds__(256) void k_compact_move(PageArgs a, const int32_t*
   }
 }
 
-// The confirmed path of each sequence's tree, from node 0 on: the next node is the first child whose
-// token is the model's choice at the present one.  One wave a sequence.
-__global__ __launch_bounds__(64) void k_tree_walk(int N, const int32_t* __restrict__ n_nodes, const int32_t* __restrict__ tokens,
-                                                  const int32_t* __restrict__ parents, const int32_t* __restrict__ chosen,
-                                                  int32_t* __restrict__ accepted, int32_t* __restrict__ n_accepted,
-                                                  int32_t* __restrict__ token_out) {
-  const int b = blockIdx.x, lane = threadIdx.x;
-  const int n = n_nodes ? min(max(n_nodes[b], 0), N) : N;
-  const int64_t row = (int64_t)b * N;
-  __shared__ int32_t tok[kMaxNodes], par[kMaxNodes], next[kMaxNodes];
-  for (int j = lane; j < n; j += 64) {
-    tok[j] = tokens[row + j];
-    par[j] = parents ? parents[row + j] : j - 1;
-    next[j] = chosen[row + j];
+// The confirmed paths of `count` trees from sequence b0 on, from node 0: the next node is the first child
+// whose token is the model's choice at the present one.  Every node offers itself to its parent (the lowest
+// wins), then a thread a tree follows the winners.  child: count * N words of LDS.
+__device__ __forceinline__ void walk_trees(const TreePick& t, int b0, int count, int32_t* child) {
+  const int N = t.N;
+  auto nodes = [&](int b) { return t.n_nodes ? min(max(t.n_nodes[b], 0), N) : N; };
+  for (int x = threadIdx.x; x < count * N; x += blockDim.x) child[x] = N;
+  __syncthreads();
+  for (int x = threadIdx.x; x < count * N; x += blockDim.x) {
+    const int s = x / N, j = x - s * N;
+    const int64_t row = (int64_t)(b0 + s) * N;
+    t.accepted[row + j] = -1;
+    if (j == 0 || j >= nodes(b0 + s)) continue;
+    const int p = t.parents ? t.parents[row + j] : j - 1;
+    if (p >= 0 && p < j && t.tokens[row + j] == t.chosen[row + p]) atomicMin(child + s * N + p, j);
   }
   __syncthreads();
-  int count = 0, cur = n > 0 ? 0 : -1, last = -1;
-  while (cur >= 0) {
-    if (lane == 0) accepted[row + count] = cur;
-    ++count;
-    last = next[cur];
-    int found = -1;
-    for (int base = (cur + 1) & ~63; base < n; base += 64) {
-      const int j = base + lane;
-      const uint64_t hit = __ballot(j > cur && j < n && par[j] == cur && tok[j] == last);
-      if (hit) {
-        found = base + __builtin_ctzll(hit);
-        break;
-      }
+  for (int s = threadIdx.x; s < count; s += blockDim.x) {
+    const int b = b0 + s;
+    int n = 0, last = -1;
+    for (int cur = nodes(b) > 0 ? 0 : N; cur < N; cur = child[s * N + cur]) {
+      t.accepted[(int64_t)b * N + n++] = cur;
+      last = cur;
     }
-    cur = found;
+    t.n_accepted[b] = n;
+    t.token_out[b] = last < 0 ? -1 : t.chosen[(int64_t)b * N + last];
   }
-  for (int j = count + lane; j < N; j += 64) accepted[row + j] = -1;
-  if (lane == 0) {
-    n_accepted[b] = count;
-    token_out[b] = last;
-  }
+  __syncthreads();
+}
+
+// Larger batches: a workgroup each kWalkWords words of nodes.
+constexpr int kWalkWords = 4096;
+__global__ __launch_bounds__(256) void k_tree_walk(TreePick t, int B) {
+  __shared__ int32_t child[kWalkWords];
+  const int per = kWalkWords / t.N, b0 = blockIdx.x * per;
+  walk_trees(t, b0, min(per, B - b0), child);
 }
 
 // Room for the confirmed tokens; a sequence without it commits nothing.
-__global__ __launch_bounds__(kPlanThreads) void k_commit_plan(PageArgs a, int B, int N, int32_t* __restrict__ accepted,
-                                                              int32_t* __restrict__ n_accepted, int32_t* __restrict__ token_out,
-                                                              int32_t* __restrict__ missing) {
+// The trees of a small batch (kWalkWords nodes) are walked here, without a launch of their own.
+template <bool WALK>
+__global__ __launch_bounds__(kPlanThreads) void k_commit_plan(PageArgs a, TreePick t, int B, int32_t* __restrict__ missing) {
   __shared__ PlanShared sh;
+  __shared__ int32_t child[WALK ? kWalkWords : 1];
+  if (WALK) walk_trees(t, 0, B, child);
   auto need = [&](int b) {
     const int at = seq_len(a, b);
-    const int64_t end = (int64_t)at + n_accepted[b];
+    const int64_t end = (int64_t)at + t.n_accepted[b];
     if (end > (int64_t)a.table_ld << a.lg) return -1;
     return pages_of(a, (int)end) - pages_of(a, at);
   };
@@ -347,11 +367,11 @@ __global__ __launch_bounds__(kPlanThreads) void k_commit_plan(PageArgs a, int B,
   });
   for (int b = threadIdx.x; b < B; b += kPlanThreads) {
     if (missing[b] == 0) {
-      a.len[b] = seq_len(a, b) + n_accepted[b];
+      a.len[b] = seq_len(a, b) + t.n_accepted[b];
     } else {
-      for (int j = 0; j < n_accepted[b]; ++j) accepted[(int64_t)b * N + j] = -1;
-      n_accepted[b] = 0;
-      token_out[b] = -1;
+      for (int j = 0; j < t.n_accepted[b]; ++j) t.accepted[(int64_t)b * t.N + j] = -1;
+      t.n_accepted[b] = 0;
+      t.token_out[b] = -1;
     }
   }
 }
@@ -404,15 +424,17 @@ hipError_t launch_compact_move(hipStream_t s, const PageArgs& a, const int32_t* 
   k_compact_move<<<copies + (a.n_seqs + 3) / 4, 256, 0, s>>>(a, ws, copies);
   return hipGetLastError();
 }
-hipError_t launch_tree_walk(hipStream_t s, int32_t B, int32_t N, const int32_t* n_nodes, const int32_t* tokens,
-                            const int32_t* parents, const int32_t* chosen, int32_t* accepted, int32_t* n_accepted,
-                            int32_t* token_out) {
-  k_tree_walk<<<B, 64, 0, s>>>(N, n_nodes, tokens, parents, chosen, accepted, n_accepted, token_out);
+bool commit_walks(int32_t B, int32_t N) { return (int64_t)B * N <= kWalkWords; }
+hipError_t launch_tree_walk(hipStream_t s, const TreePick& t, int32_t B) {
+  const int per = kWalkWords / t.N;
+  k_tree_walk<<<(B + per - 1) / per, 256, 0, s>>>(t, B);
   return hipGetLastError();
 }
-hipError_t launch_commit_plan(hipStream_t s, const PageArgs& a, int32_t B, int32_t N, int32_t* accepted, int32_t* n_accepted,
-                              int32_t* token_out, int32_t* missing) {
-  k_commit_plan<<<1, kPlanThreads, 0, s>>>(a, B, N, accepted, n_accepted, token_out, missing);
+hipError_t launch_commit_plan(hipStream_t s, const PageArgs& a, const TreePick& t, int32_t B, int32_t* missing) {
+  if (commit_walks(B, t.N))
+    k_commit_plan<true><<<1, kPlanThreads, 0, s>>>(a, t, B, missing);
+  else
+    k_commit_plan<false><<<1, kPlanThreads, 0, s>>>(a, t, B, missing);
   return hipGetLastError();
 }
 hipError_t launch_commit_rows(hipStream_t s, const PageArgs& a, int32_t B, int32_t N, const int32_t* accepted,

@@ -343,11 +343,15 @@ hipError_t launch_fork_rows(hipStream_t s, const PageArgs& a, const SeqPairs& q,
 size_t compact_words(int32_t n_pages);  // int32 words of scratch
 hipError_t launch_compact_plan(hipStream_t s, const PageArgs& a, int32_t* n_live, int32_t* ws);
 hipError_t launch_compact_move(hipStream_t s, const PageArgs& a, const int32_t* ws);
-hipError_t launch_tree_walk(hipStream_t s, int32_t B, int32_t N, const int32_t* n_nodes, const int32_t* tokens,
-                            const int32_t* parents, const int32_t* chosen, int32_t* accepted, int32_t* n_accepted,
-                            int32_t* token_out);
-hipError_t launch_commit_plan(hipStream_t s, const PageArgs& a, int32_t B, int32_t N, int32_t* accepted, int32_t* n_accepted,
-                              int32_t* token_out, int32_t* missing);
+// What a commit picks its tokens from and tells of them (arrays of B * N or B).
+struct TreePick {
+  const int32_t *n_nodes, *tokens, *parents, *chosen;
+  int32_t *accepted, *n_accepted, *token_out;
+  int32_t N;
+};
+bool commit_walks(int32_t B, int32_t N);  // the plan walks the trees itself; else launch_tree_walk comes first
+hipError_t launch_tree_walk(hipStream_t s, const TreePick& t, int32_t B);
+hipError_t launch_commit_plan(hipStream_t s, const PageArgs& a, const TreePick& t, int32_t B, int32_t* missing);
 hipError_t launch_commit_rows(hipStream_t s, const PageArgs& a, int32_t B, int32_t N, const int32_t* accepted,
                               const int32_t* n_accepted, const void* k, const void* v, int64_t layer_bytes);
 

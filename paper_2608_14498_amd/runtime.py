@@ -47,7 +47,7 @@ def _i32_dev(t: Optional[torch.Tensor], what: str, numel: Optional[int], device)
     """t as it is, checked: the C side sees an address only."""
     if t is None:
         return None
-    if t.dtype != torch.int32 or not t.is_contiguous() or t.device != device:
+    if t.dtype is not torch.int32 or not t.is_contiguous() or t.device != device:
         raise ValueError(f"{what} must be a contiguous int32 tensor on {device}")
     if numel is not None and t.numel() != numel:
         raise ValueError(f"{what} has {t.numel()} elements, not {numel}")
@@ -67,6 +67,7 @@ class PagedKV:
         if table.dim() != 2:
             raise ValueError("table is [n_seqs, table_ld]")
         self.device = k.device
+        self._index = k.get_device()
         _i32_dev(table, "table", None, self.device)
         _i32_dev(length, "length", table.shape[0], self.device)
         _i32_dev(refs, "refs", k.shape[1], self.device)
@@ -86,10 +87,11 @@ class PagedKV:
 
     def _call(self, fn, stream, *args):
         """fn(pages, stream, *args) with the pool's device current."""
-        if torch.cuda.current_device() == self.k.get_device():
-            return fn(self.pages, stream_ptr(stream), *args)
-        with torch.cuda.device(self.device):
-            return fn(self.pages, stream_ptr(stream), *args)
+        if torch.cuda.current_device() != self._index:
+            with torch.cuda.device(self.device):
+                return fn(self.pages, stream_ptr(stream), *args)
+        # (the current stream's address without a Stream object: a rollout step makes many small calls)
+        return fn(self.pages, torch._C._cuda_getCurrentRawStream(self._index) if stream is None else stream.cuda_stream, *args)
 
     def _ints(self, t, what, *shape):
         n = 1

@@ -91,7 +91,7 @@ __device__ __forceinline__ void tree_note(const TreeArgs& a, const TreeShares& s
 // Share w.  All threads of the workgroup call it.  Up to 64 sequences are cut into chunks of their own
 // where that makes a share at most `slack` tiles longer than an even cut: a second piece costs a
 // share its queries, page ids and first tiles all over again, one after the other.  8 sequences of 300 to
-// 1000 keys, 4 kv heads of 128: 18.2 us evenly cut, CHUNKED_US in chunks.
+// 1000 keys, 4 kv heads of 128: 18.2 us evenly cut, 13.8 in chunks.
 template <int NT, int KT>
 __device__ __forceinline__ TreeShares tree_find(const TreeArgs& a, int most, int least, int slack, int w, TreePiece* p) {
   __shared__ int64_t red[NT / 64];
@@ -216,23 +216,21 @@ __device__ __forceinline__ u32x4_t tree_clean(u32x4_t x) {
   return x;
 }
 
-// A score, or the lowest where it is not seen.  The empty asm keeps a branch around it a branch: the
-// compiler would mask all scores of all tiles instead, most of which are whole.
+// A score, or -inf where it is not seen: its weight is 0 by itself, as maxima are kLowest at least.  The
+// empty asm keeps a branch around it a branch: the compiler would mask all scores of all tiles
+// instead, most of which are whole.
 __device__ __forceinline__ float tree_masked(float s, bool seen) {
-  s = seen ? s : kLowest;
+  s = seen ? s : -__builtin_inff();
   asm volatile("" : "+v"(s));
   return s;
 }
 
 // The softmax step of KB blocks of 32 keys for the row of this lane: s raw scores in, weights out.
-// vis[kb]: the keys it sees (bit = key).  TAIL: cached tokens, where `some` (uniform) says that the tile
-// is not full; every row sees its first key, so a masked score's weight is 0 by itself.  DRAFT: a row
-// may see nothing, and weights are cleared one by one.
-enum TreeMask { kTail, kDraft };
-template <int DB, int KB, TreeMask MASK>
+// vis[kb]: the keys it sees (bit = key), where `some` (uniform) says that it may not see all.
+template <int DB, int KB>
 __device__ __forceinline__ void tree_softmax(f32x16_t (&s)[KB], bool some, const uint32_t (&vis)[KB], int fk, float c2, float& m,
                                              float& l, f32x16_t (&o)[DB]) {
-  if (MASK == kDraft || some) {
+  if (some) {
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -260,15 +258,14 @@ __device__ __forceinline__ void tree_softmax(f32x16_t (&s)[KB], bool some, const
   for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      float p = __builtin_amdgcn_exp2f(fmaf(s[kb][e], c2, -m));
-      if (MASK == kDraft) p = vis[kb] >> (4 * fk) >> (8 * (e >> 2) + (e & 3)) & 1 ? p : 0.f;
+      const float p = __builtin_amdgcn_exp2f(fmaf(s[kb][e], c2, -m));
       s[kb][e] = p;
       sum += p;
     }
   l += sum;
 }
 // Scores to log2 units.  A negative scale is a positive one on queries of the other sign; 0 is taken as a
-// number that a masked score times it is still far below all others.
+// tiny number, as -inf times it is to stay -inf.
 __device__ __forceinline__ float tree_c2(float scale) { return fmaxf(fabsf(scale) * 1.4426950408889634f, 1e-30f); }
 
 // Four output values of a finished row.
@@ -422,7 +419,7 @@ __device__ __forceinline__ void tree_stream(const TreeArgs& a, int shares, int l
 #pragma unroll
         for (int qi = 0; qi < QW; ++qi) {
           const uint32_t vis[1] = {cached ? tail : drafted[qi]};
-          tree_softmax<DB, 1, FIRST ? kDraft : kTail>(s[qi], there < KT, vis, fk, c2, m[qi], l[qi], o[qi]);
+          tree_softmax<DB, 1>(s[qi], !cached || there < KT, vis, fk, c2, m[qi], l[qi], o[qi]);
         }
         if (!cached) {
           bool odd = false;
@@ -674,7 +671,7 @@ void k_tree_block(TreeArgs a, int shares, int least, int slack, int RB) {
       f32x16_t s[1];
       scores(R, s[0]);
       const uint32_t vis[1] = {tree_word(a, b, ri, d, nn)};
-      tree_softmax<DB, 1, kDraft>(s, true, vis, fk, c2, m, l, o);
+      tree_softmax<DB, 1>(s, true, vis, fk, c2, m, l, o);
       u32x4_t* Vc = R + KT * CH;
       bool odd = false;  // (every wave looks at the whole tile, so that all of them agree)
 #pragma unroll 2
@@ -737,7 +734,7 @@ void k_tree_block(TreeArgs a, int shares, int least, int slack, int RB) {
           ++d;
           __syncthreads();
           copy(S0, false, d * KT, nn, 0);
-          __syncthreads();
+          tree_ring_step<0>();
         }
       }
       // Tile k.  The copies are issued past the last tile too, so that the compiler counts them exactly.
@@ -749,7 +746,7 @@ void k_tree_block(TreeArgs a, int shares, int least, int slack, int RB) {
           scores(now, s[0]);
           const int there = n0 - (from + k) * KT;
           const uint32_t vis[1] = {(1u << (there & 31)) - 1};  // (where the tile is not full)
-          tree_softmax<DB, 1, kTail>(s, there < KT, vis, fk, c2, m, l, o);
+          tree_softmax<DB, 1>(s, there < KT, vis, fk, c2, m, l, o);
           values(now, s[0]);
         }
       };

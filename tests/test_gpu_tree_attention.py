@@ -301,3 +301,42 @@ def test_in_a_graph_with_growing_lengths(dtype, N):
         graph.replay()
         torch.cuda.synchronize()
         check(dtype, out, q, [k[0][:n] for k, n in zip(K, now)], [v[0][:n] for v, n in zip(V, now)], kn, vn, now, sees, None, 128 ** -0.5)
+
+
+@pytest.mark.parametrize("dtype,Hq,N", [("bf16", 2, 1), ("f16", 8, 5), ("bf16", 8, 20), ("f32", 2, 3)])
+@pytest.mark.parametrize("scale", [0.125, 0.088, 0.1, 0.3, 2.0])
+def test_last_tile_of_infinitely_low_scores(dtype, Hq, N, scale):
+    """The only key of the last tile scores -inf for every row: the rest of the softmax stays as it is."""
+    c, K, V, kn, vn, draw, g = make(dtype, [65], N, 1, 64, 16, seed=14, layers=1)
+    q = draw(1, N, Hq, 64)
+    q[..., 0] = 1.0
+    c.k.view(-1, 64)[int(c.table[0, 4]) * 16, 0] = -math.inf
+    sees = torch.tril(torch.ones(N, N, dtype=torch.bool)).expand(1, N, N)
+    out = c.tree_attention(0, q, kn, vn, scale=scale)
+    check(dtype, out, q, [K[0][0, :64]], [V[0][0, :64]], kn, vn, [64], sees, None, scale)
+
+
+@pytest.mark.parametrize("dtype,B,N,Hq,Hkv,D", [("bf16", 70, 20, 8, 1, 64), ("f32", 80, 9, 4, 1, 128), ("f16", 66, 130, 2, 1, 128),
+                                                ("bf16", 40, 1, 8, 8, 128), ("f16", 20, 64, 16, 2, 64), ("f32", 64, 2, 8, 8, 64)])
+def test_shares_that_end_one_sequence_and_begin_the_next(dtype, B, N, Hq, Hkv, D):
+    """More sequences than lanes, or than shares."""
+    lens = [(53 * b) % 211 for b in range(B)]
+    nodes = [(b % (N + 1)) if b % 5 else N for b in range(B)]
+    c, K, V, kn, vn, draw, g = make(dtype, lens, N, Hkv, D, 16, nodes, seed=15, layers=1)
+    q = draw(B, N, Hq, D)
+    out = torch.full_like(q, 3.0)
+    sees = tree(B, N, g)
+    c.tree_attention(0, q, kn, vn, mask=words(sees), n_nodes=torch.tensor(nodes, dtype=torch.int32, device="cuda"), out=out)
+    check(dtype, out, q, [k[0] for k in K], [v[0] for v in V], kn, vn, lens, sees, nodes, D ** -0.5, torch.full_like(q, 3.0))
+
+
+def test_drafted_tiles_of_large_trees_side_by_side():
+    """Eight drafted tiles a sequence and hardly any cached ones: the stages are filled again and again."""
+    lens = [0, 3, 40, 0, 33]
+    c, K, V, kn, vn, draw, g = make("bf16", lens, 250, 2, 128, 8, seed=16, layers=1)
+    q = draw(5, 250, 14, 128)
+    sees = tree(5, 250, g, back=40)
+    want = c.tree_attention(0, q, kn, vn, mask=words(sees))
+    check("bf16", want, q, [k[0] for k in K], [v[0] for v in V], kn, vn, lens, sees, None, 128 ** -0.5)
+    for _ in range(3):
+        assert torch.equal(c.tree_attention(0, q, kn, vn, mask=words(sees)), want)

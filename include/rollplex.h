@@ -361,7 +361,7 @@ rp_status rp_decode_step_static(const rp_model *model, void *stream, int32_t B, 
  * rp_pages_append  row r of rows (packed [R][n_kv_heads][head_dim] per layer, as
  *   rp_prefix_forward leaves kv_out; layer_stride elements apart), cu[i] <= r <
  *   cu[i+1], becomes the next token of sequence seqs[i] (cu: host int32 [n+1],
- *   cu[0] = 0, non-decreasing; rows may be NULL where cu[n] = 0).
+ *   cu[0] = 0, non-decreasing, cu[n] <= 2^30; rows may be NULL where cu[n] = 0).
  * rp_pages_fork    sequence dst[i] gives its pages back and becomes a copy of
  *   src[i]: full pages are shared, the rows of a last, partial one are copied to a
  *   page of its own.  All dst are freed before the first page is taken; a dst that

@@ -175,9 +175,10 @@ def _ptr(x) -> Optional[int]:
 def _i32(seq: Optional[Sequence[int]]):
     if seq is None:
         return None
+    seq = list(seq)
     try:
         vals = array("i", seq)
-    except (TypeError, OverflowError):  # not a sequence of whole numbers that fit
+    except (TypeError, OverflowError):  # not whole numbers that fit
         vals = [int(v) for v in seq]
         return (c_int32 * len(vals))(*vals)
     return (c_int32 * len(vals)).from_buffer(vals) if vals else (c_int32 * 0)()

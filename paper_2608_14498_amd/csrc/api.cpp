@@ -1396,6 +1396,7 @@ rp_status rp_pages_append(const rp_pages* pages, void* stream, int32_t n, const 
   if (cu[0] != 0) return fail(RP_ERR_SHAPE, "cu[0] = %d, must be 0", cu[0]);
   for (int i = 0; i < n; ++i)
     if (cu[i + 1] < cu[i]) return fail(RP_ERR_SHAPE, "cu[%d] = %d < cu[%d] = %d", i + 1, cu[i + 1], i, cu[i]);
+  if (cu[n] > 1 << 30) return fail(RP_ERR_UNSUPPORTED, "cu[%d] = %d rows > 2^30", n, cu[n]);
   if ((st = check_rows(*pages, rows, cu[n], "rows")) != RP_OK) return st;
   hipStream_t s = (hipStream_t)stream;
   const rp::PageArgs a = page_args(*pages);

@@ -93,11 +93,27 @@ class PagedKV:
         # (the current stream's address without a Stream object: a rollout step makes many small calls)
         return fn(self.pages, torch._C._cuda_getCurrentRawStream(self._index) if stream is None else stream.cuda_stream, *args)
 
-    def _ints(self, t, what, *shape):
+    def _empty(self, stream, shape, dtype=torch.int32) -> torch.Tensor:
+        """A tensor of the stream that the call runs on: its memory is handed on behind that call."""
+        if stream is None:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(stream):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def _ints(self, t, what, stream, *shape):
+        if t is None:
+            return self._empty(stream, shape)
         n = 1
         for x in shape:
             n *= x
-        return torch.empty(shape, dtype=torch.int32, device=self.device) if t is None else _i32_dev(t, what, n, self.device)
+        return _i32_dev(t, what, n, self.device)
+
+    def _workspace(self, ws, stream, nbytes):
+        if ws is None:
+            return self._empty(stream, max(nbytes(), 256), torch.uint8)
+        if ws.dtype is not torch.uint8 or not ws.is_contiguous() or ws.device != self.device:
+            raise ValueError(f"workspace must be a contiguous uint8 tensor on {self.device}")
+        return ws
 
     def _rows(self, K, V, rows: int) -> rb.RpKV:
         """Packed rows [L, ..., Hkv, Dh] of the pool's type."""
@@ -114,7 +130,7 @@ class PagedKV:
         seqs[i].  Returns missing [n]: 0, or why sequence i stayed as it was (rollplex.h)."""
         if len(cu) != len(seqs) + 1:
             raise ValueError("cu has one entry more than seqs")
-        missing = self._ints(missing, "missing", len(seqs))
+        missing = self._ints(missing, "missing", stream, len(seqs))
         self._call(rb.rp_pages_append, stream, len(seqs), seqs, cu, self._rows(K, V, int(cu[-1])), missing)
         return missing
 
@@ -122,7 +138,7 @@ class PagedKV:
         """Sequence dst[i] gives its pages back and becomes a copy of src[i] that shares its full pages."""
         if len(src) != len(dst):
             raise ValueError("src and dst have the same length")
-        missing = self._ints(missing, "missing", len(dst))
+        missing = self._ints(missing, "missing", stream, len(dst))
         self._call(rb.rp_pages_fork, stream, len(dst), src, dst, missing)
         return missing
 
@@ -134,8 +150,8 @@ class PagedKV:
 
     def compact(self, n_live=None, workspace=None, stream=None) -> torch.Tensor:
         """Moves the pages in use to the lowest ids; returns their number (int32 [1])."""
-        n_live = self._ints(n_live, "n_live", 1)
-        ws = workspace if workspace is not None else self.compact_workspace()
+        n_live = self._ints(n_live, "n_live", stream, 1)
+        ws = self._workspace(workspace, stream, lambda: rb.rp_pages_compact_workspace_bytes(self.pages))
         self._call(rb.rp_pages_compact, stream, n_live, ws, ws.numel())
         return n_live
 
@@ -159,12 +175,12 @@ class PagedKV:
             if t.shape != (B, N, H, D) or t.dtype != q.dtype or t.device != self.device or not t.is_contiguous():
                 raise ValueError(f"k_new and v_new are contiguous [{B}, {N}, {H}, {D}] of the pool's type and device")
         if out is None:
-            out = torch.empty((B, N, Hq, D), dtype=q.dtype, device=self.device)
+            out = self._empty(stream, (B, N, Hq, D), q.dtype)
         elif out.shape != q.shape or out.dtype != q.dtype or out.device != self.device or not out.is_contiguous():
             raise ValueError("out is contiguous, of q's shape, type and device")
         _i32_dev(mask, "mask", B * N * ((N + 31) // 32), self.device)
         _i32_dev(n_nodes, "n_nodes", B, self.device)
-        ws = workspace if workspace is not None else self.attention_workspace(B, N, Hq)
+        ws = self._workspace(workspace, stream, lambda: rb.rp_tree_attention_workspace_bytes(self.pages, B, N, Hq))
         self._call(rb.rp_tree_attention, stream, layer, B, N, Hq, n_nodes, mask, q, q_ld, k_new, v_new,
                    D ** -0.5 if scale is None else scale, out, ws, ws.numel())
         return out
@@ -177,9 +193,9 @@ class PagedKV:
         for t, what in ((token_ids, "token_ids"), (parents, "parents"), (next_ids, "next_ids")):
             _i32_dev(t, what, B * N, self.device)
         _i32_dev(n_nodes, "n_nodes", B, self.device)
-        accepted = self._ints(accepted, "accepted", B, N)
-        n_accepted, token_out = self._ints(n_accepted, "n_accepted", B), self._ints(token_out, "token_out", B)
-        missing = self._ints(missing, "missing", B)
+        accepted = self._ints(accepted, "accepted", stream, B, N)
+        n_accepted, token_out = self._ints(n_accepted, "n_accepted", stream, B), self._ints(token_out, "token_out", stream, B)
+        missing = self._ints(missing, "missing", stream, B)
         self._call(rb.rp_tree_commit, stream, B, N, n_nodes, token_ids, parents, next_ids, self._rows(K, V, B * N),
                    accepted, n_accepted, token_out, missing)
         return accepted, n_accepted, token_out, missing
@@ -320,16 +336,18 @@ class DeviceModel:
         parents [B, N]; None: chains).  Returns (next_ids [B, N], K, V [L, B * N, Hkv, Dh] of the new tokens,
         for PagedKV.commit)."""
         B, N = token_ids.shape
+        if cache.device != self.embed.device:
+            raise ValueError(f"the cache is on {cache.device}, the model on {self.embed.device}")
         for t, what, n in ((token_ids, "token_ids", B * N), (parents, "parents", B * N), (n_nodes, "n_nodes", B),
                            (pos0, "pos0", B), (next_ids, "next_ids", B * N)):
             _i32_dev(t, what, n, cache.device)
         if logits is not None and (logits.dtype != torch.float32 or logits.numel() != B * N * self.shape.vocab or
-                                   not logits.is_contiguous()):
+                                   not logits.is_contiguous() or logits.device != cache.device):
             raise ValueError("logits is a contiguous float32 tensor [B, N, V]")
-        K, V = draft if draft is not None else self.alloc_kv(B * N)
-        if next_ids is None:
-            next_ids = torch.empty((B, N), dtype=torch.int32, device=self.device)
-        ws = workspace if workspace is not None else self.workspace(rb.rp_tree_step_workspace_bytes(self.handle, B, N))
+        K, V = draft if draft is not None else [
+            cache._empty(stream, (cache.k.shape[0], B * N) + cache.k.shape[3:], cache.k.dtype) for _ in "kv"]
+        next_ids = cache._ints(next_ids, "next_ids", stream, B, N)
+        ws = cache._workspace(workspace, stream, lambda: rb.rp_tree_step_workspace_bytes(self.handle, B, N))
         rows = cache._rows(K, V, B * N)
         cache._call(lambda pages, st: rb.rp_tree_step(self.handle, st, pages, B, N, n_nodes, token_ids, parents, pos0,
                                                       rows, logits, next_ids, ws, ws.numel()), stream)

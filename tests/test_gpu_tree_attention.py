@@ -340,3 +340,20 @@ def test_drafted_tiles_of_large_trees_side_by_side():
     check("bf16", want, q, [k[0] for k in K], [v[0] for v in V], kn, vn, lens, sees, None, 128 ** -0.5)
     for _ in range(3):
         assert torch.equal(c.tree_attention(0, q, kn, vn, mask=words(sees)), want)
+
+
+def test_own_workspace_on_another_stream():
+    """A call on another stream leaves its workspace to that stream: what is allocated next on this one is elsewhere."""
+    c, K, V, kn, vn, draw, g = make("bf16", [4000], 2, 2, 128, 16, seed=17, layers=1)
+    q = draw(1, 2, 14, 128)
+    sees = torch.tril(torch.ones(2, 2, dtype=torch.bool)).expand(1, 2, 2)
+    n = c.attention_workspace(1, 2, 14).numel()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+    out = c.tree_attention(0, q, kn, vn, stream=side)
+    over = [torch.full((n,), 0x7F, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    torch.cuda.synchronize()
+    check("bf16", out, q, [K[0][0]], [V[0][0]], kn, vn, [4000], sees, None, 128 ** -0.5)
+    assert all((t == 0x7F).all() for t in over)

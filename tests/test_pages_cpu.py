@@ -92,6 +92,13 @@ def test_append_and_fork_refusals():
     refused(rb.RP_ERR_SHAPE, "both a src and a dst", rb.rp_pages_fork, p, 0, 2, [0, 1], [2, 0], FAKE)
     refused(rb.RP_ERR_SHAPE, "both a src and a dst", rb.rp_pages_fork, p, 0, 1, [3], [3], FAKE)
     refused(rb.RP_ERR_INVALID_ARG, "missing", rb.rp_pages_fork, p, 0, 1, [0], [1], None)
+    huge = [0, (1 << 30) + 1]
+    refused(rb.RP_ERR_UNSUPPORTED, "2\\^30", rb.rp_pages_append, p, 0, 1, [0], huge, rb.make_kv(FAKE, FAKE, 1 << 40), FAKE)
+
+
+@pytest.mark.parametrize("seq", [[3, 1], (3, 1), b"\x03\x01", iter([3, 1]), [3.0, 1.0], iter([3, 1.5]), torch.tensor([3, 1])])
+def test_host_lists_of_any_kind(seq):
+    assert list(rb._i32(seq)) == [3, 1]
 
 
 def test_compact_workspace():
@@ -206,6 +213,10 @@ def test_python_layer_checks_shapes_and_types():
         c.tree_attention(0, q, n, n, mask=torch.zeros(2, 3, 1, dtype=torch.int64))
     with pytest.raises(ValueError, match="out"):
         c.tree_attention(0, q, n, n, out=q[:1])
+    with pytest.raises(ValueError, match="workspace"):
+        c.tree_attention(0, q, n, n, workspace=torch.zeros(1 << 20))
+    with pytest.raises(ValueError, match="workspace"):
+        c.compact(workspace=torch.zeros(1 << 20, dtype=torch.int32))
     ids = torch.zeros(2, 3, dtype=torch.int32)
     with pytest.raises(ValueError, match="parents"):
         c.commit(ids, ids[:1], ids, K, K)

@@ -31,11 +31,7 @@ struct PlanShared {
 // Inclusive scan of one value a thread over the workgroup; *total: the sum.
 __device__ __forceinline__ int block_scan(int v, int32_t* wave, int* total) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int u = __shfl_up(v, o, 64);
-    if (lane >= o) v += u;
-  }
+  v = wave_scan(v);
   __syncthreads();
   if (lane == 63) wave[w] = v;
   __syncthreads();
@@ -212,7 +208,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_fork_plan(PageArgs a, SeqPairs
   __shared__ PlanShared sh;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   for (int i = w; i < q.n; i += kPlanWaves) release(a, q.dst[i], lane);
-  __threadfence();
+  __builtin_amdgcn_s_waitcnt(0);  // the counts are down; (a fence of the device's scope took 3 us)
   __syncthreads();
   const int in_page = (1 << a.lg) - 1;
   take_pages(a, q.n, sh, missing, [&](int i) { return (seq_len(a, q.src[i]) & in_page) ? 1 : 0; },
@@ -290,7 +286,6 @@ __global__ __launch_bounds__(kPlanThreads) void k_compact_plan(PageArgs a, int32
     holes += sum & 0xffff;
     movers += sum >> 16;
   }
-  __threadfence();
   __syncthreads();
   for (int i = threadIdx.x; i < movers; i += kPlanThreads) {
     const int f = from[i], t = to[i];

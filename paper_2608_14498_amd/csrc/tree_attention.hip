@@ -105,19 +105,11 @@ __device__ __forceinline__ TreeShares tree_find(const TreeArgs& a, int most, int
   if (a.few) {  // every wave by itself, a sequence a lane
     const int lane = threadIdx.x & 63;
     const int mine = lane < a.B ? tree_tiles<KT>(a, lane) : 0;
-    auto scan = [&](int v) {
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const int x = __shfl_up(v, o, 64);
-        if (lane >= o) v += x;
-      }
-      return v;
-    };
-    const int incl = scan(mine), total = __builtin_amdgcn_readlane(incl, 63);
+    const int incl = wave_scan(mine), total = __builtin_amdgcn_readlane(incl, 63);
     TreeShares sh = even(total);
     const int ideal = (total + sh.shares - 1) / sh.shares;
     for (int c = ideal; c <= ideal + slack && total > 0; c += 1 + c / 16) {
-      const int cuts = (mine + c - 1) / c, ci = scan(cuts), n = __builtin_amdgcn_readlane(ci, 63);
+      const int cuts = (mine + c - 1) / c, ci = wave_scan(cuts), n = __builtin_amdgcn_readlane(ci, 63);
       if (n > most) continue;
       sh.shares = n;
       sh.chunk = c;
@@ -990,6 +982,7 @@ __global__ __launch_bounds__(64 * TM_WAVES) void k_tree_merge(TreeArgs a, int BQ
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int G = a.Hq / a.Hkv, groups = (a.N * G + TM_WAVES * ROWS - 1) / (TM_WAVES * ROWS);
   const int r0 = (blockIdx.x % groups * TM_WAVES + wave) * ROWS, g = blockIdx.x / groups % a.Hkv, b = blockIdx.x / groups / a.Hkv;
+  const int2 held = a.held[b];  // (of a sequence without rows: whatever, and not used)
   const int rows = tree_nodes(a, b) * G;
   auto out_at = [&](int r) {
     const int i = r / G;
@@ -1002,18 +995,25 @@ __global__ __launch_bounds__(64 * TM_WAVES) void k_tree_merge(TreeArgs a, int BQ
     }
   }
   if (r0 >= rows) return;
-  const int2 held = a.held[b];
   const int wa = __builtin_amdgcn_readfirstlane(held.x), wb = __builtin_amdgcn_readfirstlane(held.y);
   if (wa == wb) return;  // one share held it all
   auto record = [&](int w, int rb) { return a.part + tree_record_at(a, w, w == wa, g, rb, RB, BQ); };
   if constexpr (ROWS == 1) {
+    auto across = [&](float x, auto f) {  // f over the wave, in lane moves and four reads of lanes
+      x = f(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0xB1, 0xf, 0xf, false)));   // quad_perm 1,0,3,2
+      x = f(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x4E, 0xf, 0xf, false)));   // quad_perm 2,3,0,1
+      x = f(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x124, 0xf, 0xf, false)));  // row_ror 4
+      x = f(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x128, 0xf, 0xf, false)));  // row_ror 8
+      auto row = [&](int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), l)); };
+      return f(f(row(0), row(16)), f(row(32), row(48)));
+    };
     const int rb = r0 / BQ, in = r0 - rb * BQ;
     float M = kLowest, L = 0.f;
     vec_t o = {};
     for (int base = wa; base <= wb; base += 64) {
       float2 x = make_float2(kLowest, 0.f);
       if (base + lane <= wb) x = *reinterpret_cast<const float2*>(record(base + lane, rb) + BQ * D + 2 * in);
-      const float mn = fmaxf(M, wave_max(x.x)), old = __builtin_amdgcn_exp2f(M - mn);
+      const float mn = fmaxf(M, across(x.x, [](float p, float q) { return fmaxf(p, q); })), old = __builtin_amdgcn_exp2f(M - mn);
       const float f = __builtin_amdgcn_exp2f(x.x - mn);
       M = mn;
       L = fmaf(x.y, f, L * old);
@@ -1034,7 +1034,7 @@ __global__ __launch_bounds__(64 * TM_WAVES) void k_tree_merge(TreeArgs a, int BQ
         }
       }
     }
-    const float inv = tree_inv(wave_sum(L));
+    const float inv = tree_inv(across(L, [](float p, float q) { return p + q; }));
 #pragma unroll
     for (int c = 0; c < PER; ++c) {
       const float y = (o[c] + __shfl_xor(o[c], 32, kWave)) * inv;

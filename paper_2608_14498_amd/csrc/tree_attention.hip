@@ -107,7 +107,7 @@ __device__ __forceinline__ TreeShares tree_find(const TreeArgs& a, int most, int
     const int mine = lane < a.B ? tree_tiles<KT>(a, lane) : 0;
     const int incl = wave_scan(mine), total = __builtin_amdgcn_readlane(incl, 63);
     TreeShares sh = even(total);
-    const int ideal = (total + sh.shares - 1) / sh.shares;
+    const int ideal = max(least, (total + most - 1) / most);
     for (int c = ideal; c <= ideal + slack && total > 0; c += 1 + c / 16) {
       const int cuts = (mine + c - 1) / c, ci = wave_scan(cuts), n = __builtin_amdgcn_readlane(ci, 63);
       if (n > most) continue;
@@ -1145,7 +1145,7 @@ static TreePlan tree_plan(rp_dtype dt, int32_t N, int32_t Hq, int32_t Hkv) {
   // a stream workgroup has a CU's LDS to itself, of the others two share one
   p.shares = (p.stream ? 256 : 512) / (Hkv * p.RB);
   if (p.shares < 1) p.shares = 1;
-  p.least = p.stream ? 3 : 4;
+  p.least = dt == RP_F32 ? 1 : p.stream ? 3 : 4;
   p.slack = p.stream ? 24 : 8;
   return p;
 }

@@ -90,8 +90,9 @@ __device__ __forceinline__ void tree_note(const TreeArgs& a, const TreeShares& s
 
 // Share w.  All threads of the workgroup call it.  Up to 64 sequences are cut into chunks of their own
 // where that makes a share at most `slack` tiles longer than an even cut: a second piece costs a
-// share its queries, page ids and first tiles all over again, one after the other.  8 sequences of 300 to
-// 1000 keys, 4 kv heads of 128: 18.2 us evenly cut, 13.8 in chunks.
+// share its queries, page ids and first tiles all over again, one after the other.  4 kv heads of 128, evenly
+// cut and in chunks: 8 sequences of 300 to 1000 keys 17.1 and 11.5 us, 32 of 100 to 2000 keys 25.5 and
+// 22.0; 6 trees of 7 tokens over 300 keys in fp32 16.4 and 13.4.
 template <int NT, int KT>
 __device__ __forceinline__ TreeShares tree_find(const TreeArgs& a, int most, int least, int slack, int w, TreePiece* p) {
   __shared__ int64_t red[NT / 64];
@@ -233,7 +234,8 @@ __device__ __forceinline__ void tree_softmax(f32x16_t (&s)[KB], bool some, const
   for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
     for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[kb][e]);
-  mx = fmaxf(mx, __shfl_xor(mx, 32, kWave)) * c2;
+  const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+  mx = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * c2;
   // raised only where some lane's maximum grows by more than 2^kLazy: numerator and sum share it
   if (__any(mx > m + kLazy)) {
     const float mn = fmaxf(m, mx);
@@ -279,6 +281,9 @@ __device__ __forceinline__ float tree_inv(float l) { return l == 0.f ? 0.f : 1.0
 // (two tiles of 16 KB in flight a wave; no barrier inside a piece), and join their sums in LDS at the
 // piece's end.  S^T = K Q^T and O^T += V^T P^T with v_mfma_f32_32x32x16 as in the prefix kernel:
 // a lane holds one row's scores.  A wave's page ids are read 64 tiles ahead, a lane each.
+// 64 x 8192 keys, 4 kv heads of 128: 193 us, 5.6 TB/s.  One tile and one sequence: 9.5 us, of which
+// finding the share 3, the queries and the first tile 3, the rest mostly the fetch of code that runs
+// once, to judge by early exits; one sequence of 4000 keys 10.7 (and 5.2 for the merge).
 // ------------------------------------------------------------------------------------
 constexpr int TS_WAVES = 3;
 template <typename T16, int D, int QW, bool SMALL>
@@ -563,7 +568,15 @@ __global__ __launch_bounds__(64 * TS_WAVES) void k_tree_stream64(TreeArgs a, int
 // More rows (large trees).  A workgroup's four waves hold 32 rows each and share tiles of 32 keys in a ring
 // of four stages; two workgroups share a CU.  One barrier a tile: behind it the tile has landed for every
 // wave and the one before has been read by all, so its stage takes the copies of the tile three further
-// on.
+// on.  The K fragments are read all at once (the compiler would wait for each), V's during the softmax.
+//
+// 112 rows over 32 x 8192 keys: 129 us, 4.2 TB/s, near what the copies alone take.  448 rows over 8 x
+// 16384: 168 us, 0.72 PFLOP/s, where a SIMD's two waves spend 45% of the time on products and 41% on
+// the softmax, hardly at once.  Tried and left: 64 rows a wave (the sums spill); eight waves a barrier (all
+// wait for the slowest: 10% slower); tiles of 64 keys (two stages fit two workgroups: the copies come
+// too late); scores a tile ahead (no gain); eight waves of 32 rows in two groups half a tile apart,
+// one at the products while the other is at the softmax (448 rows 161 us, but 320 rows 300 instead of 262: the
+// second block of 256 is filled to a quarter).
 // ------------------------------------------------------------------------------------
 template <int N>
 __device__ __forceinline__ void tree_ring_step() {  // this wave's copies but the last N have landed; all waves are here
@@ -631,37 +644,43 @@ void k_tree_block(TreeArgs a, int shares, int least, int slack, int RB) {
       for (int e = 0; e < 16; ++e) o[db][e] = 0.f;
 
     // s[e] = score(key 8(e/4) + 4 fk + e%4 of the tile in R, row fr)
-    auto scores = [&](const u32x4_t* R, f32x16_t& s) __attribute__((always_inline)) {
+    auto read_k = [&](const u32x4_t* R, V8 (&kf)[KSTEPS]) __attribute__((always_inline)) {
 #pragma unroll
-      for (int ks = 0; ks < KSTEPS; ++ks) {
-        const V8 kf = __builtin_bit_cast(V8, R[fr * CH + ((ks * 2 + fk) ^ kswz<D>(fr))]);
-        s = H::mma(kf, qf[ks], ks == 0 ? f32x16_t{} : s);
+      for (int ks = 0; ks < KSTEPS; ++ks) kf[ks] = __builtin_bit_cast(V8, R[fr * CH + ((ks * 2 + fk) ^ kswz<D>(fr))]);
+    };
+    auto scores = [&](const V8 (&kf)[KSTEPS], f32x16_t& s) __attribute__((always_inline)) {
+#pragma unroll
+      for (int ks = 0; ks < KSTEPS; ++ks) s = H::mma(kf[ks], qf[ks], ks == 0 ? f32x16_t{} : s);
+    };
+    // o += V^T P^T
+    auto read_v = [&](const u32x4_t* R, V8 (&vf)[2 * DB]) __attribute__((always_inline)) {
+      const T16* vbase = reinterpret_cast<const T16*>(R + KT * CH);
+#pragma unroll
+      for (int i = 0; i < 2 * DB; ++i) {
+        const int ka = i / DB * 16 + tr_key, kc = ka + 8, col = i % DB * 32 + tr_col;
+        const int ca = ((col >> 3) ^ vswz<D>(ka)) * 8 + (col & 7);
+        const int cc = ((col >> 3) ^ vswz<D>(kc)) * 8 + (col & 7);
+        const v4i16_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t*)(vbase + ka * D + ca));
+        const v4i16_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t*)(vbase + kc * D + cc));
+        const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
+        vf[i] = H::as_v8(make_uint4(l2.x, l2.y, h2.x, h2.y));
       }
     };
-    // o += V^T P^T of the tile in R
-    auto values = [&](const u32x4_t* R, const f32x16_t& x) __attribute__((always_inline)) {
-      const T16* vbase = reinterpret_cast<const T16*>(R + KT * CH);
+    auto values = [&](const V8 (&vf)[2 * DB], const f32x16_t& x) __attribute__((always_inline)) {
 #pragma unroll
       for (int hh = 0; hh < 2; ++hh) {
         const V8 pf = H::as_v8(make_uint4(H::pack2(x[hh * 8 + 0], x[hh * 8 + 1]), H::pack2(x[hh * 8 + 2], x[hh * 8 + 3]),
                                           H::pack2(x[hh * 8 + 4], x[hh * 8 + 5]), H::pack2(x[hh * 8 + 6], x[hh * 8 + 7])));
-        const int ka = hh * 16 + tr_key, kc = ka + 8;
 #pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          const int col = db * 32 + tr_col;
-          const int ca = ((col >> 3) ^ vswz<D>(ka)) * 8 + (col & 7);
-          const int cc = ((col >> 3) ^ vswz<D>(kc)) * 8 + (col & 7);
-          const v4i16_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t*)(vbase + ka * D + ca));
-          const v4i16_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t*)(vbase + kc * D + cc));
-          const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
-          o[db] = H::mma(H::as_v8(make_uint4(l2.x, l2.y, h2.x, h2.y)), pf, o[db]);
-        }
+        for (int db = 0; db < DB; ++db) o[db] = H::mma(vf[hh * DB + db], pf, o[db]);
       }
     };
     // Drafted tile d from R, whole.
     auto draft = [&](u32x4_t* R, int d) __attribute__((always_inline)) {
       f32x16_t s[1];
-      scores(R, s[0]);
+      V8 kf[KSTEPS], vf[2 * DB];
+      read_k(R, kf);
+      scores(kf, s[0]);
       const uint32_t vis[1] = {tree_word(a, b, ri, d, nn)};
       tree_softmax<DB, 1>(s, true, vis, fk, c2, m, l, o);
       u32x4_t* Vc = R + KT * CH;
@@ -678,7 +697,8 @@ void k_tree_block(TreeArgs a, int shares, int least, int slack, int RB) {
         for (int j = 0; j < LOADS; ++j) Vc[(wave * LOADS + j) * 64 + lane] = tree_clean<T16>(Vc[(wave * LOADS + j) * 64 + lane]);
         __syncthreads();
       }
-      values(R, s[0]);
+      read_v(R, vf);
+      values(vf, s[0]);
     };
     // Copies this wave's KW of the tokens from `first` on, of n (cached: in page `page`).
     auto copy = [&](u32x4_t* R, bool cached, int first, int n, int page) __attribute__((always_inline)) {
@@ -729,17 +749,22 @@ void k_tree_block(TreeArgs a, int shares, int least, int slack, int RB) {
           tree_ring_step<0>();
         }
       }
-      // Tile k.  The copies are issued past the last tile too, so that the compiler counts them exactly.
+      // Tile k; false behind the last.  (No branch around the copies, whose issue goes between the products; the
+      // compiler counts them exactly.)
       auto step = [&](u32x4_t* next, const u32x4_t* now, int k) __attribute__((always_inline)) {
         tree_ring_step<(NS - 2) * 2 * LOADS>();
+        V8 kf[KSTEPS], vf[2 * DB];
+        read_k(now, kf);
+        __builtin_amdgcn_sched_barrier(0);
         load(next, k + NS - 1);
         if (k < n) {
           f32x16_t s[1];
-          scores(now, s[0]);
+          scores(kf, s[0]);
+          read_v(now, vf);
           const int there = n0 - (from + k) * KT;
           const uint32_t vis[1] = {(1u << (there & 31)) - 1};  // (where the tile is not full)
           tree_softmax<DB, 1>(s, there < KT, vis, fk, c2, m, l, o);
-          values(now, s[0]);
+          values(vf, s[0]);
         }
       };
       for (int k = 0; k < n; k += NS) {
@@ -778,7 +803,9 @@ void k_tree_block(TreeArgs a, int shares, int least, int slack, int RB) {
 // ------------------------------------------------------------------------------------
 // fp32 on the fp32 matrix cores (v_mfma_f32_32x32x2: exact products), blocks of 32 rows whose NW waves
 // take the tiles of 32 keys in turn, fragments straight from global memory as in the prefix's fp32
-// kernel, and join their sums in LDS.
+// kernel, and join their sums in LDS.  6 trees of 7 tokens over up to 577 keys (64): 10.4 us, a chain of
+// loads (lengths, page ids, K, V) and 64 products of 64 cycles; 16 trees of 20 tokens over 3000 to 4000 keys
+// (128): 74 us, 45 TFLOP/s.
 // ------------------------------------------------------------------------------------
 template <int D, int NW>
 __global__ __launch_bounds__(NW * 64) void k_tree_f32(TreeArgs a, int shares, int least, int slack, int RB) {
@@ -971,7 +998,8 @@ __global__ __launch_bounds__(NW * 64) void k_tree_f32(TreeArgs a, int shares, in
 // Bound by latency (which shares, their maxima and sums, their o: three loads in a row), so a wave has
 // many of each in flight.  Few rows (one sequence in many shares): a wave a row, its halves taking
 // every other record.  Many rows (few shares each): eight rows a wave, a lane for each of their
-// maxima, each half taking every other row.
+// maxima, each half taking every other row.  One and eight rows a wave: 28 rows of 42 records 5.2 and 17 us,
+// 280 of 64 7.6 and 18.8, 1792 of one 5.0 and 4.8, 3584 of two to five 12.5 and 8.3, 20480 of four 21.8 and 11.2.
 // ------------------------------------------------------------------------------------
 constexpr int TM_WAVES = 4, TM_MANY = 8;
 template <typename T, int D, int ROWS>
@@ -1131,6 +1159,15 @@ __global__ __launch_bounds__(kMaxNodes) void k_tree_plan(int N, int W, const int
 
 // How a launch runs: rows of a block (QW groups of 32 a wave), row blocks, shares of the tiles (a share:
 // one workgroup per kv head and row block), the least tiles of one, and how much longer chunks may be.
+// Measured, main kernel + merge in us (4 kv heads of 128 but for fp32):
+//   stream or blocks of 128 rows: 64 sequences of one token over 8192 keys 192 + 5 or 225 + 7, 16 of 4 tokens
+//   over 4000 29.6 + 4.7 or 31.4 + 5.0, 16 of 9 tokens (63 rows) 34.5 + 5.7 or 33.3 + 6.3.
+//   32 or 64 rows a wave, 7 rows: 192 or 201 as above, 8 sequences of 300 to 1000 keys 13.4 or 16.1.
+//   Shares: twice as many make the 16 of 4 tokens 38.0, 112 rows of 32 mixed trees 81 + 13 instead of 71 + 8.
+//   Least tiles: one sequence of 4000 keys, 1, 3, 6, 12 tiles: 11.1 + 6.5, 10.7 + 5.1, 12.1 + 4.3, 13.4 + 3.8; 4
+//   trees of 224 rows over 500 to 900 keys, 1, 4, 8, 16: 16.6 + 6.7, 16.1 + 5.3, 18.7 + 5.3, 24.2 + 4.8; fp32, 6
+//   trees over 300 keys, 1, 4, 8: 10.2, 13.4, 17.0.
+//   Slack: a third of it makes the 32 mixed trees 74.6 + 9.6, three times as much changes nothing.
 struct TreePlan {
   bool stream;
   int QW, BQ, RB, shares, least, slack;
@@ -1164,7 +1201,7 @@ hipError_t launch_tree_attention(hipStream_t s, rp_dtype dt, const TreeArgs& arg
   a.held = reinterpret_cast<int2*>(a.part + tree_records(p, a.Hkv, a.D));
   typedef std::integral_constant<int, 128> D128;
   typedef std::integral_constant<int, 64> D64;
-  // up to four rows a wave slot of the chip: a wave a row
+  // up to four rows a wave slot of the chip: a wave a row (k_tree_merge has both measured)
   const int rows = a.N * (a.Hq / a.Hkv), per = (int64_t)rows * a.Hkv * a.B <= 4096 ? 1 : TM_MANY;
   const int64_t merge = (int64_t)((rows + TM_WAVES * per - 1) / (TM_WAVES * per)) * a.Hkv * a.B;
   auto join = [&](auto t_, auto d_) {
@@ -1192,6 +1229,8 @@ hipError_t launch_tree_attention(hipStream_t s, rp_dtype dt, const TreeArgs& arg
       constexpr int D = decltype(d_)::value;
       if (p.stream) {
         const int grid = p.shares * a.Hkv;
+        // pages of 8 or 16 tokens: a tile in groups of 8 keys, each from its own page (as many buffer
+        // resources again: the 64 sequences of 8192 keys 198 us instead of 193)
         const bool small = a.lg < 5;
         if (p.QW == 1)
           small ? k_tree_stream32<T, D, true><<<grid, 64 * TS_WAVES, 0, s>>>(a, p.shares, p.least, p.slack)

@@ -369,7 +369,8 @@ __global__ __launch_bounds__(256) void k_tree_walk(TreePick t, int B) {
 }
 
 // Room for the confirmed tokens; a sequence without it commits nothing.
-// The trees of a small batch (kWalkWords nodes) are walked here, without a launch of their own.
+// The trees of a small batch (kWalkWords nodes) are walked here, without a launch of their own: 64 trees of 16
+// nodes 5.2 us instead of 3.9 + 3.4, 64 of 64 nodes 7.5 instead of 10.0 + 3.6.
 template <bool WALK>
 __global__ __launch_bounds__(kPlanThreads) void k_commit_plan(PageArgs a, TreePick t, int B, int32_t* __restrict__ missing) {
   __shared__ PlanShared sh;

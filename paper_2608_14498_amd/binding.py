@@ -172,13 +172,15 @@ def _ptr(x) -> Optional[int]:
     return x.data_ptr()
 
 
-def _i32(seq: Optional[Sequence[int]]):
+def _i32(seq: Optional[Sequence[int]], wrap: bool = True):
     if seq is None:
         return None
     seq = list(seq)
     try:
         vals = array("i", seq)
     except (TypeError, OverflowError):  # not whole numbers that fit
+        if not wrap and any(not -(1 << 31) <= int(v) < 1 << 31 for v in seq):
+            raise ValueError("a listed number does not fit 32 bits")
         vals = [int(v) for v in seq]
         return (c_int32 * len(vals))(*vals)
     return (c_int32 * len(vals)).from_buffer(vals) if vals else (c_int32 * 0)()
@@ -310,15 +312,15 @@ def make_pages(k, v, layer_stride: int, dtype: str, n_layers: int, n_kv_heads: i
 
 
 def rp_pages_append(pages: RpPages, stream, n: int, seqs, cu, rows: RpKV, missing) -> None:
-    _check(lib().rp_pages_append(byref(pages), _ptr(stream), int(n), _i32(seqs), _i32(cu), rows, _ptr(missing)))
+    _check(lib().rp_pages_append(byref(pages), _ptr(stream), int(n), _i32(seqs, False), _i32(cu, False), rows, _ptr(missing)))
 
 
 def rp_pages_fork(pages: RpPages, stream, n: int, src, dst, missing) -> None:
-    _check(lib().rp_pages_fork(byref(pages), _ptr(stream), int(n), _i32(src), _i32(dst), _ptr(missing)))
+    _check(lib().rp_pages_fork(byref(pages), _ptr(stream), int(n), _i32(src, False), _i32(dst, False), _ptr(missing)))
 
 
 def rp_pages_free(pages: RpPages, stream, n: int, seqs) -> None:
-    _check(lib().rp_pages_free(byref(pages), _ptr(stream), int(n), _i32(seqs)))
+    _check(lib().rp_pages_free(byref(pages), _ptr(stream), int(n), _i32(seqs, False)))
 
 
 def rp_pages_compact_workspace_bytes(pages: RpPages) -> int:

@@ -15,7 +15,7 @@ TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
 
 class Both:
     """A pool on the GPU beside its model.  Token x's key in layer l is the number x + l / 4 in every
-    element (v: its negative), exact in the types for the numbers used."""
+    element (v: its negative), rounded to the type."""
 
     def __init__(self, dtype, n_pages, page, n_seqs, table_ld, L=2, H=2, D=64):
         self.gpu = PagedKV.empty(L, n_pages, page, H, D, n_seqs, table_ld, dtype=TYPES[dtype])
@@ -51,6 +51,7 @@ class Both:
         for b, row in enumerate(m.table):
             for t in range(m.len[b]):
                 hold[row[t // m.page], t % m.page] = True
+        want = want.to(g.k.dtype)  # (as rows() rounded them: 64.25 needs nine bits, bf16 has eight)
         assert torch.equal(g.k.cpu().double()[:, hold], want.double()[:, hold])
         assert torch.equal(g.v.cpu().double()[:, hold], -want.double()[:, hold])
 
@@ -229,3 +230,8 @@ def test_calls_in_a_graph():
         torch.cuda.synchronize()
         for x, y in zip(state(), want):
             assert torch.equal(x, y), rep
+
+
+@pytest.mark.parametrize("N,B", [(256, 16), (256, 17), (64, 64), (64, 65)])
+def test_commit_at_the_most_nodes_of_one_workgroup(N, B):
+    test_commit("bf16", N, B)

@@ -357,3 +357,44 @@ def test_own_workspace_on_another_stream():
     torch.cuda.synchronize()
     check("bf16", out, q, [K[0][0]], [V[0][0]], kn, vn, [4000], sees, None, 128 ** -0.5)
     assert all((t == 0x7F).all() for t in over)
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,D,N,lens", [("f16", 300, 300, 64, 1, [70, 0, 333]), ("bf16", 80, 40, 64, 250, [90, 17]),
+                                                   ("f32", 600, 600, 64, 1, [40, 3]), ("bf16", 96, 96, 128, 70, [45, 0, 100])])
+def test_more_heads_than_shares(dtype, Hq, Hkv, D, N, lens):
+    """One share or a few hold everything."""
+    c, K, V, kn, vn, draw, g = make(dtype, lens, N, Hkv, D, 16, seed=18, layers=1)
+    q = draw(len(lens), N, Hq, D)
+    sees = tree(len(lens), N, g)
+    out = c.tree_attention(0, q, kn, vn, mask=words(sees))
+    check(dtype, out, q, [k[0] for k in K], [v[0] for v in V], kn, vn, lens, sees, None, D ** -0.5)
+
+
+@pytest.mark.parametrize("dtype,N,Hq,Hkv", [("bf16", 1, 28, 4), ("bf16", 16, 28, 4), ("f32", 7, 4, 2)])
+def test_one_workspace_in_two_graphs(dtype, N, Hq, Hkv):
+    """Two captured calls share a workspace and are replayed in turn, with eager calls between them."""
+    lens = [[1500, 3, 400], [10, 2900, 0]]
+    made = [make(dtype, n, N, Hkv, 128, 32, seed=19 + i, layers=1) for i, n in enumerate(lens)]
+    qs = [m[5](3, N, Hq, 128) for m in made]
+    ws = made[0][0].attention_workspace(3, N, Hq)
+    outs = [torch.zeros_like(q) for q in qs]
+    sees = torch.tril(torch.ones(N, N, dtype=torch.bool)).expand(3, N, N)
+    call = lambda i: made[i][0].tree_attention(0, qs[i], made[i][3], made[i][4], out=outs[i], workspace=ws)
+    want = [call(i).clone() for i in range(2)]
+    graphs, side = [torch.cuda.CUDAGraph() for _ in range(2)], torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for i in range(2):
+        with torch.cuda.stream(side):
+            with torch.cuda.graph(graphs[i], stream=side):
+                call(i)
+    torch.cuda.current_stream().wait_stream(side)
+    for rep in range(3):
+        for i in (0, 1, 1, 0):
+            outs[i].zero_()
+            graphs[i].replay()
+            call(1 - i)
+            torch.cuda.synchronize()
+            assert torch.equal(outs[i], want[i]) and torch.equal(outs[1 - i], want[1 - i]), (rep, i)
+    for i in range(2):
+        c, K, V, kn, vn = made[i][:5]
+        check(dtype, want[i], qs[i], [k[0] for k in K], [v[0] for v in V], kn, vn, lens[i], sees, None, 128 ** -0.5)

@@ -101,6 +101,16 @@ def test_host_lists_of_any_kind(seq):
     assert list(rb._i32(seq)) == [3, 1]
 
 
+def test_listed_numbers_that_do_not_fit():
+    """(They would wrap round to another sequence.)"""
+    p = pages()
+    for call, args in ((rb.rp_pages_append, (1, [1 << 32], [0, 1], ROWS, FAKE)), (rb.rp_pages_append, (1, [0], [0, 1 << 32], ROWS, FAKE)),
+                       (rb.rp_pages_fork, (1, [1 << 32], [1], FAKE)), (rb.rp_pages_fork, (1, [1], [1 << 32], FAKE)),
+                       (rb.rp_pages_free, (1, [-(1 << 32)]))):
+        with pytest.raises(ValueError, match="32 bits"):
+            call(p, 0, *args)
+
+
 def test_compact_workspace():
     need = rb.rp_pages_compact_workspace_bytes(pages())
     assert 2 * 64 * 4 <= need <= 4 * 64 * 4

@@ -722,6 +722,7 @@ void k_tree_block(TreeArgs a, int shares, int least, int slack, int RB) {
     int drafts = t1 - max(t0, P0);
     for (int from = t0; from < te || drafts > 0; from += 128) {
       const int n = min(te - from, 128);
+      const int work = rb * BQ + wave * 32 < rows ? n : 0;  // a wave past the last row only copies
       int pid[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -757,7 +758,7 @@ void k_tree_block(TreeArgs a, int shares, int least, int slack, int RB) {
         read_k(now, kf);
         __builtin_amdgcn_sched_barrier(0);
         load(next, k + NS - 1);
-        if (k < n) {
+        if (k < work) {
           f32x16_t s[1];
           scores(kf, s[0]);
           read_v(now, vf);

@@ -402,12 +402,14 @@ __device__ __forceinline__ void tree_stream(const TreeArgs& a, int shares, int l
         constexpr bool FIRST = decltype(first_)::value;
         u32x4_t *Kc = R, *Vc = R + KT * CH;
         f32x16_t s[QW][1];
+        V8 kf[KSTEPS];  // (read at once: the compiler would wait for each)
 #pragma unroll
-        for (int ks = 0; ks < KSTEPS; ++ks) {
-          const V8 kf = __builtin_bit_cast(V8, Kc[fr * CH + ((ks * 2 + fk) ^ kswz<D>(fr))]);
+        for (int ks = 0; ks < KSTEPS; ++ks) kf[ks] = __builtin_bit_cast(V8, Kc[fr * CH + ((ks * 2 + fk) ^ kswz<D>(fr))]);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int qi = 0; qi < QW; ++qi) s[qi][0] = H::mma(kf, qf[qi][ks], ks == 0 ? f32x16_t{} : s[qi][0]);
-        }
+        for (int ks = 0; ks < KSTEPS; ++ks)
+#pragma unroll
+          for (int qi = 0; qi < QW; ++qi) s[qi][0] = H::mma(kf[ks], qf[qi][ks], ks == 0 ? f32x16_t{} : s[qi][0]);
         // s[qi][0][e] = score(key 8(e/4) + 4 fk + e%4, row fr)
         const bool cached = !FIRST || i >= 0;
         const int there = n0 - (ts + NW * i) * KT;

@@ -178,14 +178,14 @@ __device__ __forceinline__ uint4 flip_sign(uint4 v, uint32_t flip) {
 // Drafted values that are not numbers: a weight of 0 would not keep them from rows that do not see
 // their token.  Rows that do see it take them here, as they are (their weight is positive);
 // the tile is then cleaned of them (tree_clean) and multiplied as any other.
-// vis: tokens key0 .. key0 + 31 that this lane's row sees; V rows of 8-element chunks swizzled by vswz.
+// vis: the tile's tokens that this lane's row sees; V rows of 8-element chunks swizzled by vswz.
 template <typename T16, int D>
-__device__ __forceinline__ void tree_odd_values(const T16* v, int key0, uint32_t vis, int fk, f32x16_t (&o)[D / 32]) {
+__device__ __forceinline__ void tree_odd_values(const T16* v, uint32_t vis, int fk, f32x16_t (&o)[D / 32]) {
   typedef Half16<T16> H;
   auto odd = [](float x, bool seen) { return seen && !(fabsf(x) <= 3.4028235e38f) ? x : 0.f; };
 #pragma unroll 1
-  for (int key = key0; key < key0 + 32; ++key) {
-    const bool seen = vis >> (key - key0) & 1;
+  for (int key = 0; key < 32; ++key) {
+    const bool seen = vis >> key & 1;
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
 #pragma unroll
@@ -218,22 +218,18 @@ __device__ __forceinline__ float tree_masked(float s, bool seen) {
   return s;
 }
 
-// The softmax step of KB blocks of 32 keys for the row of this lane: s raw scores in, weights out.
-// vis[kb]: the keys it sees (bit = key), where `some` (uniform) says that it may not see all.
-template <int DB, int KB>
-__device__ __forceinline__ void tree_softmax(f32x16_t (&s)[KB], bool some, const uint32_t (&vis)[KB], int fk, float c2, float& m,
-                                             float& l, f32x16_t (&o)[DB]) {
+// The softmax step of 32 keys for the row of this lane: s raw scores in, weights out.
+// vis: the keys it sees (bit = key), where `some` (uniform) says that it may not see all.
+template <int DB>
+__device__ __forceinline__ void tree_softmax(f32x16_t& s, bool some, uint32_t vis, int fk, float c2, float& m, float& l,
+                                             f32x16_t (&o)[DB]) {
   if (some) {
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[kb][e] = tree_masked(s[kb][e], vis[kb] >> (4 * fk) >> (8 * (e >> 2) + (e & 3)) & 1);
+    for (int e = 0; e < 16; ++e) s[e] = tree_masked(s[e], vis >> (4 * fk) >> (8 * (e >> 2) + (e & 3)) & 1);
   }
   float mx = kLowest;
 #pragma unroll
-  for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[kb][e]);
+  for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[e]);
   const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
   mx = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * c2;
   // raised only where some lane's maximum grows by more than 2^kLazy: numerator and sum share it
@@ -249,13 +245,10 @@ __device__ __forceinline__ void tree_softmax(f32x16_t (&s)[KB], bool some, const
   }
   float sum = 0.f;
 #pragma unroll
-  for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const float p = __builtin_amdgcn_exp2f(fmaf(s[kb][e], c2, -m));
-      s[kb][e] = p;
-      sum += p;
-    }
+  for (int e = 0; e < 16; ++e) {
+    s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c2, -m));
+    sum += s[e];
+  }
   l += sum;
 }
 // Scores to log2 units.  A negative scale is a positive one on queries of the other sign; 0 is taken as a
@@ -401,7 +394,7 @@ __device__ __forceinline__ void tree_stream(const TreeArgs& a, int shares, int l
       auto tile = [&](u32x4_t* R, int i, auto first_) __attribute__((always_inline)) {
         constexpr bool FIRST = decltype(first_)::value;
         u32x4_t *Kc = R, *Vc = R + KT * CH;
-        f32x16_t s[QW][1];
+        f32x16_t s[QW];
         V8 kf[KSTEPS];  // (read at once: the compiler would wait for each)
 #pragma unroll
         for (int ks = 0; ks < KSTEPS; ++ks) kf[ks] = __builtin_bit_cast(V8, Kc[fr * CH + ((ks * 2 + fk) ^ kswz<D>(fr))]);
@@ -409,17 +402,15 @@ __device__ __forceinline__ void tree_stream(const TreeArgs& a, int shares, int l
 #pragma unroll
         for (int ks = 0; ks < KSTEPS; ++ks)
 #pragma unroll
-          for (int qi = 0; qi < QW; ++qi) s[qi][0] = H::mma(kf[ks], qf[qi][ks], ks == 0 ? f32x16_t{} : s[qi][0]);
+          for (int qi = 0; qi < QW; ++qi) s[qi] = H::mma(kf[ks], qf[qi][ks], ks == 0 ? f32x16_t{} : s[qi]);
         // s[qi][0][e] = score(key 8(e/4) + 4 fk + e%4, row fr)
         const bool cached = !FIRST || i >= 0;
         const int there = n0 - (ts + NW * i) * KT;
         const uint32_t tail = there >= KT ? ~0u : (1u << (there & 31)) - 1;
         const T16* vbase = reinterpret_cast<const T16*>(Vc);
 #pragma unroll
-        for (int qi = 0; qi < QW; ++qi) {
-          const uint32_t vis[1] = {cached ? tail : drafted[qi]};
-          tree_softmax<DB, 1>(s[qi], !cached || there < KT, vis, fk, c2, m[qi], l[qi], o[qi]);
-        }
+        for (int qi = 0; qi < QW; ++qi)
+          tree_softmax<DB>(s[qi], !cached || there < KT, cached ? tail : drafted[qi], fk, c2, m[qi], l[qi], o[qi]);
         if (!cached) {
           bool odd = false;
 #pragma unroll
@@ -429,7 +420,7 @@ __device__ __forceinline__ void tree_stream(const TreeArgs& a, int shares, int l
           }
           if (__any(odd)) {
 #pragma unroll
-            for (int qi = 0; qi < QW; ++qi) tree_odd_values<T16, D>(vbase, 0, drafted[qi], fk, o[qi]);
+            for (int qi = 0; qi < QW; ++qi) tree_odd_values<T16, D>(vbase, drafted[qi], fk, o[qi]);
 #pragma unroll
             for (int j = 0; j < LOADS; ++j) Vc[j * 64 + lane] = tree_clean<T16>(Vc[j * 64 + lane]);
           }
@@ -439,7 +430,7 @@ __device__ __forceinline__ void tree_stream(const TreeArgs& a, int shares, int l
           V8 pf[QW];
 #pragma unroll
           for (int qi = 0; qi < QW; ++qi) {
-            const f32x16_t& x = s[qi][0];
+            const f32x16_t& x = s[qi];
             pf[qi] = H::as_v8(make_uint4(H::pack2(x[hh * 8 + 0], x[hh * 8 + 1]), H::pack2(x[hh * 8 + 2], x[hh * 8 + 3]),
                                          H::pack2(x[hh * 8 + 4], x[hh * 8 + 5]), H::pack2(x[hh * 8 + 6], x[hh * 8 + 7])));
           }
@@ -679,12 +670,12 @@ void k_tree_block(TreeArgs a, int shares, int least, int slack, int RB) {
     };
     // Drafted tile d from R, whole.
     auto draft = [&](u32x4_t* R, int d) __attribute__((always_inline)) {
-      f32x16_t s[1];
+      f32x16_t s;
       V8 kf[KSTEPS], vf[2 * DB];
       read_k(R, kf);
-      scores(kf, s[0]);
-      const uint32_t vis[1] = {tree_word(a, b, ri, d, nn)};
-      tree_softmax<DB, 1>(s, true, vis, fk, c2, m, l, o);
+      scores(kf, s);
+      const uint32_t vis = tree_word(a, b, ri, d, nn);
+      tree_softmax<DB>(s, true, vis, fk, c2, m, l, o);
       u32x4_t* Vc = R + KT * CH;
       bool odd = false;  // (every wave looks at the whole tile, so that all of them agree)
 #pragma unroll 2
@@ -693,14 +684,14 @@ void k_tree_block(TreeArgs a, int shares, int least, int slack, int RB) {
         odd |= not_finite<T16>(x[0]) || not_finite<T16>(x[1]) || not_finite<T16>(x[2]) || not_finite<T16>(x[3]);
       }
       if (__any(odd)) {
-        tree_odd_values<T16, D>(reinterpret_cast<const T16*>(Vc), 0, vis[0], fk, o);
+        tree_odd_values<T16, D>(reinterpret_cast<const T16*>(Vc), vis, fk, o);
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) Vc[(wave * LOADS + j) * 64 + lane] = tree_clean<T16>(Vc[(wave * LOADS + j) * 64 + lane]);
         __syncthreads();
       }
       read_v(R, vf);
-      values(vf, s[0]);
+      values(vf, s);
     };
     // Copies this wave's KW of the tokens from `first` on, of n (cached: in page `page`).
     auto copy = [&](u32x4_t* R, bool cached, int first, int n, int page) __attribute__((always_inline)) {
@@ -761,13 +752,12 @@ void k_tree_block(TreeArgs a, int shares, int least, int slack, int RB) {
         __builtin_amdgcn_sched_barrier(0);
         load(next, k + NS - 1);
         if (k < work) {
-          f32x16_t s[1];
-          scores(kf, s[0]);
+          f32x16_t s;
+          scores(kf, s);
           read_v(now, vf);
           const int there = n0 - (from + k) * KT;
-          const uint32_t vis[1] = {(1u << (there & 31)) - 1};  // (where the tile is not full)
-          tree_softmax<DB, 1>(s, there < KT, vis, fk, c2, m, l, o);
-          values(vf, s[0]);
+          tree_softmax<DB>(s, there < KT, (1u << (there & 31)) - 1, fk, c2, m, l, o);
+          values(vf, s);
         }
       };
       for (int k = 0; k < n; k += NS) {

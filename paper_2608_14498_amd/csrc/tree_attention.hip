@@ -92,7 +92,9 @@ __device__ __forceinline__ void tree_note(const TreeArgs& a, const TreeShares& s
 // where that makes a share at most `slack` tiles longer than an even cut: a second piece costs a
 // share its queries, page ids and first tiles all over again, one after the other.  4 kv heads of 128, evenly
 // cut and in chunks: 8 sequences of 300 to 1000 keys 17.1 and 11.5 us, 32 of 100 to 2000 keys 25.5 and
-// 22.0; 6 trees of 7 tokens over 300 keys in fp32 16.4 and 13.4.
+// 22.0; 6 trees of 7 tokens over 300 keys in fp32 16.4 and 13.4.  As many shares as there are and 64 for one
+// sequence (kernel + merge, one kv head): 8800 keys of 64 in fp32 16.6 + 16.2 and 13.4 + 4.8, 60000 of
+// 128 in bf16 14.6 + 16.2 and 17.0 + 5.9, 8000 of them 9.8 + 7.5 and 10.4 + 5.6.
 template <int NT, int KT>
 __device__ __forceinline__ TreeShares tree_find(const TreeArgs& a, int most, int least, int slack, int w, TreePiece* p) {
   __shared__ int64_t red[NT / 64];
@@ -108,7 +110,8 @@ __device__ __forceinline__ TreeShares tree_find(const TreeArgs& a, int most, int
     const int mine = lane < a.B ? tree_tiles<KT>(a, lane) : 0;
     const int incl = wave_scan(mine), total = __builtin_amdgcn_readlane(incl, 63);
     TreeShares sh = even(total);
-    const int ideal = max(least, (total + most - 1) / most);
+    // no more than 64 shares a sequence on the average, which a wave of the merge takes at once
+    const int per = min(most, 64 * a.B), ideal = max(least, (total + per - 1) / per);
     for (int c = ideal; c <= ideal + slack && total > 0; c += 1 + c / 16) {
       const int cuts = (mine + c - 1) / c, ci = wave_scan(cuts), n = __builtin_amdgcn_readlane(ci, 63);
       if (n > most) continue;
@@ -276,7 +279,7 @@ __device__ __forceinline__ float tree_inv(float l) { return l == 0.f ? 0.f : 1.0
 // a lane holds one row's scores.  A wave's page ids are read 64 tiles ahead, a lane each.
 // 64 x 8192 keys, 4 kv heads of 128: 193 us, 5.6 TB/s.  One tile and one sequence: 9.5 us, of which
 // finding the share 3, the queries and the first tile 3, the rest mostly the fetch of code that runs
-// once, to judge by early exits; one sequence of 4000 keys 10.7 (and 5.2 for the merge).
+// once, as early exits show; one sequence of 4000 keys 10.7 (and 5.2 for the merge).
 // ------------------------------------------------------------------------------------
 constexpr int TS_WAVES = 3;
 template <typename T16, int D, int QW, bool SMALL>

@@ -398,3 +398,14 @@ def test_one_workspace_in_two_graphs(dtype, N, Hq, Hkv):
     for i in range(2):
         c, K, V, kn, vn = made[i][:5]
         check(dtype, want[i], qs[i], [k[0] for k in K], [v[0] for v in V], kn, vn, lens[i], sees, None, 128 ** -0.5)
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,D,N,lens", [("f32", 2, 1, 64, 2, [8800]), ("bf16", 4, 1, 128, 1, [20000]), ("f32", 2, 1, 64, 1, [30, 9000]),
+                                                   ("bf16", 4, 1, 64, 40, [9000])])
+def test_one_long_sequence_in_many_shares(dtype, Hq, Hkv, D, N, lens):
+    """Up to 64 records a sequence, and more where lengths differ."""
+    c, K, V, kn, vn, draw, g = make(dtype, lens, N, Hkv, D, 16, seed=20, layers=1)
+    q = draw(len(lens), N, Hq, D)
+    sees = tree(len(lens), N, g)
+    out = c.tree_attention(0, q, kn, vn, mask=words(sees))
+    check(dtype, out, q, [k[0] for k in K], [v[0] for v in V], kn, vn, lens, sees, None, D ** -0.5)

@@ -341,8 +341,9 @@ rp_status rp_decode_step_static(const rp_model *model, void *stream, int32_t B, 
  *   table   int32 [n_seqs][table_ld]; entries past a sequence's pages are not read
  *   len     int32 [n_seqs]: tokens held; ceil(len/page_size) entries are in use
  *   refs    int32 [n_pages]: table entries in use that hold the page, 0 = free
- * page_size is a power of two in [8, 1024] and table_ld*page_size < 2^31.  An
- * empty pool is len = 0 and refs = 0.  A full page may be shared; the page that a
+ * page_size is a power of two in [8, 1024], table_ld*page_size <= 2^31 - 2^14 and
+ * n_pages*page_size < 2^31 (else RP_ERR_UNSUPPORTED).  An empty pool is len = 0 and
+ * refs = 0.  A full page may be shared; the page that a
  * sequence writes next never is.  The calls enqueue kernels only (no allocation,
  * copy or synchronisation), so they can be captured in a HIP graph.  Calls that
  * change one pool are ordered by the caller (one stream, or events).  Lengths

@@ -1243,6 +1243,11 @@ rp_status rp_decode_step_static(const rp_model* m, void* stream, int32_t B, rp_k
 
 namespace {
 
+// Tokens that a sequence's table may hold.  Lengths on the device are clamped to it and counted in 32 bits, rounded
+// up to a page (1023 more at most) or a tile, and the attention's page ids are looked up ahead of a wave's present
+// tile: by 127 tiles of 32 tokens (blocks), or by 63 of three waves in turn (one to 64 rows), 6240 tokens with the rest.
+constexpr int64_t kMaxSeqTokens = ((int64_t)1 << 31) - (1 << 14);
+
 rp_status check_pages(const rp_pages* p) {
   if (!p) return fail(RP_ERR_INVALID_ARG, "pages is NULL");
   int dt = 0;  // (see check_config)
@@ -1258,8 +1263,9 @@ rp_status check_pages(const rp_pages* p) {
     return fail(RP_ERR_SHAPE, "pages: page_size %d is not a power of two in [8, 1024]", p->page_size);
   const int64_t row = (int64_t)p->n_kv_heads * p->head_dim, es = dt == RP_F32 ? 4 : 2;
   if (row > (1 << 20) || row * es % 16) return fail(RP_ERR_UNSUPPORTED, "pages: rows must be 16-byte multiples of at most 2^20 elements");
-  if ((int64_t)p->table_ld * p->page_size >= (int64_t)1 << 31)
-    return fail(RP_ERR_UNSUPPORTED, "pages: table_ld * page_size must be below 2^31");
+  if ((int64_t)p->table_ld * p->page_size > kMaxSeqTokens)
+    return fail(RP_ERR_UNSUPPORTED, "pages: table_ld * page_size %lld > 2^31 - 2^14",
+                (long long)p->table_ld * p->page_size);
   if (p->n_layers > 32767 || (int64_t)p->n_pages * p->page_size >= (int64_t)1 << 31)
     return fail(RP_ERR_UNSUPPORTED, "pages: too many layers or tokens");
   if (p->kv.layer_stride < (int64_t)p->n_pages * p->page_size * row)

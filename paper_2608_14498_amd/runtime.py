@@ -168,7 +168,8 @@ class PagedKV:
         if q.dim() != 4 or q.shape[3] != D or q.dtype != self.k.dtype or q.device != self.device:
             raise ValueError(f"q is [B, N, Hq, {D}] of the pool's type and device")
         B, N, Hq, _ = q.shape
-        if q.stride(3) != 1 or q.stride(2) != D or (B > 1 and q.stride(0) != N * q.stride(1)):
+        # (the stride of a dimension of one element says nothing)
+        if q.stride(3) != 1 or (Hq > 1 and q.stride(2) != D) or (B > 1 and N > 1 and q.stride(0) != N * q.stride(1)):
             raise ValueError("q: heads must be contiguous and rows evenly spaced")
         q_ld = q.stride(1) if N > 1 else q.stride(0) if B > 1 else Hq * D
         for t in (k_new, v_new):

@@ -179,11 +179,12 @@ __device__ __forceinline__ void copy_bytes(uint8_t* __restrict__ dst, const uint
 
 // One row a wave: row r of the packed rows goes to its sequence's token len - rows + (r - cu[i]).
 // Four prompts of 4096 tokens, 4 layers (134 MB): 47 us, 5.6 TB/s read and written.
+// A launch takes the rows from `first` on (launch_append_rows; a loop over rows in here took those prompts 5 us more).
 __global__ __launch_bounds__(256) void k_append_rows(PageArgs a, SeqRows q, const uint8_t* __restrict__ k,
                                                      const uint8_t* __restrict__ v, int64_t layer_bytes,
-                                                     const int32_t* __restrict__ missing) {
+                                                     const int32_t* __restrict__ missing, int first) {
   const int lane = threadIdx.x & 63;
-  const int r = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+  const int r = first + __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
   if (r >= q.cu[q.n]) return;
   int lo = 0, hi = q.n - 1;
   while (lo < hi) {
@@ -418,8 +419,13 @@ hipError_t launch_append_plan(hipStream_t s, const PageArgs& a, const SeqRows& q
 }
 hipError_t launch_append_rows(hipStream_t s, const PageArgs& a, const SeqRows& q, const void* k, const void* v,
                               int64_t layer_bytes, const int32_t* missing) {
+  // a launch has fewer than 2^32 threads in x; with more it runs their number modulo 2^32, without an error
+  constexpr int kMostRows = 1 << 24;
   const int rows = q.cu[q.n];
-  k_append_rows<<<dim3((rows + 3) / 4, a.n_layers, 2), 256, 0, s>>>(a, q, (const uint8_t*)k, (const uint8_t*)v, layer_bytes, missing);
+  for (int first = 0; first < rows; first += kMostRows) {
+    const int groups = (std::min(rows - first, kMostRows) + 3) / 4;
+    k_append_rows<<<dim3(groups, a.n_layers, 2), 256, 0, s>>>(a, q, (const uint8_t*)k, (const uint8_t*)v, layer_bytes, missing, first);
+  }
   return hipGetLastError();
 }
 hipError_t launch_pages_free(hipStream_t s, const PageArgs& a, const SeqRows& q) {

@@ -1,0 +1,29 @@
+"""Paged cache calls of more rows or sequences than one launch has threads for."""
+import pytest
+import torch
+
+from paper_2608_14498_amd.runtime import PagedKV
+
+pytestmark = pytest.mark.gpu
+
+
+def numbered(n, start=0):
+    """[1, n, 1, 8] rows of 16 bytes that hold their number (as four int32)."""
+    return torch.arange(start, start + n, dtype=torch.int32, device="cuda").repeat_interleave(4).view(torch.bfloat16).view(1, n, 1, 8)
+
+
+def test_append_of_more_rows_than_waves_of_one_launch():
+    """2^26 rows and some at a wave a row: 2^32 threads."""
+    first, second = (1 << 26) - 700, 711
+    n = first + second
+    c = PagedKV.empty(1, (n + 1023) // 1024 + 2, 1024, 1, 8, 2, (first + 1023) // 1024, dtype=torch.bfloat16)
+    k, v = numbered(n), numbered(n, 1 << 27)
+    print(f"[pages] append of {n} rows", flush=True)
+    assert c.append([1, 0], [0, first, n], k, v).tolist() == [0, 0]
+    assert c.length.tolist() == [second, first]
+    assert int(c.refs.sum()) == (first + 1023) // 1024 + 1
+    slots = lambda pool, b, m: pool.view(-1, 1024, 8)[c.table[b, :(m + 1023) // 1024].long()].view(-1, 8)[:m].view(torch.int32)
+    for pool, rows in ((c.k, k), (c.v, v)):
+        rows = rows.view(n, 8).view(torch.int32)
+        assert torch.equal(slots(pool, 1, first), rows[:first])
+        assert torch.equal(slots(pool, 0, second), rows[first:])

@@ -305,17 +305,18 @@ __global__ __launch_bounds__(kPlanThreads) void k_compact_plan(PageArgs a, int32
   }
 }
 
-// New ids in the tables (blocks beyond the first `copies`), and the moved pages' contents.
+// New ids in the tables (blocks beyond the first `copies`, a wave a sequence and then further ones), and the moved
+// pages' contents.
 __global__ __launch_bounds__(256) void k_compact_move(PageArgs a, const int32_t* __restrict__ ws, int copies) {
   const int32_t *map = ws + 1, *from = map + a.n_pages, *to = from + a.n_pages / 2;
   if ((int)blockIdx.x >= copies) {
-    const int seq = (blockIdx.x - copies) * 4 + (threadIdx.x >> 6);
-    if (seq >= a.n_seqs) return;
-    const int n = pages_of(a, seq_len(a, seq));
-    int32_t* row = a.table + (int64_t)seq * a.table_ld;
-    for (int j = threadIdx.x & 63; j < n; j += 64) {
-      const int id = row[j];
-      if (id >= 0 && id < a.n_pages) row[j] = map[id];
+    for (int64_t seq = (blockIdx.x - copies) * 4 + (threadIdx.x >> 6); seq < a.n_seqs; seq += 4 * ((int)gridDim.x - copies)) {
+      const int n = pages_of(a, seq_len(a, (int)seq));
+      int32_t* row = a.table + seq * a.table_ld;
+      for (int j = threadIdx.x & 63; j < n; j += 64) {
+        const int id = row[j];
+        if (id >= 0 && id < a.n_pages) row[j] = map[id];
+      }
     }
     return;
   }
@@ -447,7 +448,8 @@ hipError_t launch_compact_plan(hipStream_t s, const PageArgs& a, int32_t* n_live
 }
 hipError_t launch_compact_move(hipStream_t s, const PageArgs& a, const int32_t* ws) {
   const int copies = (int)std::min<int64_t>(2048, (int64_t)(a.n_pages / 2 + 1) * a.n_layers * 2);
-  k_compact_move<<<copies + (a.n_seqs + 3) / 4, 256, 0, s>>>(a, ws, copies);
+  const int tables = (int)std::min<int64_t>(1 << 16, ((int64_t)a.n_seqs + 3) / 4);  // (2^32 threads run as none)
+  k_compact_move<<<copies + tables, 256, 0, s>>>(a, ws, copies);
   return hipGetLastError();
 }
 bool commit_walks(int32_t B, int32_t N) { return (int64_t)B * N <= kWalkWords; }

@@ -397,7 +397,9 @@ rp_status rp_pages_compact(const rp_pages *pages, void *stream, int32_t *n_live,
  * sequence costs little more than one).  Batch entry b is table row b, b < B <=
  * n_seqs; it has n_nodes[b] new tokens (dev int32 [B], clamped to [0, N]; NULL =
  * N) in rows b*N .. of arrays of B*N rows, N in [1, RP_MAX_NODES]; rows past
- * n_nodes[b] are padding.
+ * n_nodes[b] are padding.  B*N <= 2^24 (a step: B*N < 2^22), and for the attention
+ * B * n_kv_heads * ceil(N*group/32) < 2^24 with group = n_q_heads / n_kv_heads, else
+ * RP_ERR_UNSUPPORTED.
  *
  * rp_tree_attention  grouped-query attention of the new tokens of one layer: row i
  *   of b attends to the len[b] cached tokens and to the new tokens j < n_nodes[b]

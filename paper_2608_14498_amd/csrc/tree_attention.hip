@@ -867,15 +867,17 @@ __global__ __launch_bounds__(NW * 64) void k_tree_f32(TreeArgs a, int shares, in
       if (!cached) vis = tree_word(a, b, ri, t - P0, nn);
       float vf[DB][16];
       const float* vb = (const float*)(cached ? a.v : a.vn) + g * D;
-      auto v_row = [&](int key) {  // key 8 j + ..: the page is lane 8 j's
-        const int pg = __builtin_amdgcn_readlane(page, key & 24);
-        return cached ? ((int64_t)pg << a.lg) + ((first + (key & 24)) & ((1 << a.lg) - 1)) : row0 + first + (key & 24);
-      };
+      // Row of key 8 j: keys 8 j .. 8 j + 7 lie in one page, lane 8 j's.  (A lane's own choice is made among rows, not
+      // among lanes to ask for a page.)  Past the last key the first one is read, and not used.
+      int64_t at[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        at[j] = cached ? ((int64_t)__builtin_amdgcn_readlane(page, 8 * j) << a.lg) + ((first + 8 * j) & ((1 << a.lg) - 1)) : row0 + first + 8 * j;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const int in = 4 * fk + (e & 3), key = 8 * (e >> 2) + in;
         const bool is = key < cnt;
-        const float* vp = vb + (v_row(8 * (is ? (e >> 2) : 0)) + (is ? in : 0)) * ld + fr;
+        const float* vp = vb + ((is ? at[e >> 2] : at[0]) + (is ? in : 0)) * ld + fr;
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
           const float x = vp[db * 32];

@@ -221,9 +221,21 @@ __device__ __forceinline__ float tree_masked(float s, bool seen) {
   return s;
 }
 
+// Weights are 2^(score - m), rounded to the 16-bit type for the value product (the sum takes them unrounded): an error of
+// half a step of a weight, as the output's own rounding is of the output.  fp16 has no such half steps below 2^-14 and
+// nothing below 2^-25, so m is kept kLift under the row's maximum there: weights down to 2^-20 of the largest are rounded by
+// half a step and smaller ones by at most 2^-31 of it, 2^-12 of the row over 2^19 keys; and with up to 2^kSlack more before
+// m is raised the largest is 2^12.  (With m at the maximum 2^18 keys whose weights are 2^-25.2 of one of them lost
+// their 0.6% of the row.  A slack of 4 beside a lift of 7: 320 rows over 8 x 16384 keys 1% slower; 6 and 6: no slower.)
+template <typename T16>
+struct TreeRange {
+  static constexpr bool half = std::is_same<T16, f16_t>::value;
+  static constexpr float kLift = half ? 6.f : 0.f, kSlack = half ? 6.f : kLazy;
+};
+
 // The softmax step of 32 keys for the row of this lane: s raw scores in, weights out.
 // vis: the keys it sees (bit = key), where `some` (uniform) says that it may not see all.
-template <int DB>
+template <typename T16, int DB>
 __device__ __forceinline__ void tree_softmax(f32x16_t& s, bool some, uint32_t vis, int fk, float c2, float& m, float& l,
                                              f32x16_t (&o)[DB]) {
   if (some) {
@@ -234,9 +246,9 @@ __device__ __forceinline__ void tree_softmax(f32x16_t& s, bool some, uint32_t vi
 #pragma unroll
   for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[e]);
   const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-  mx = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * c2;
-  // raised only where some lane's maximum grows by more than 2^kLazy: numerator and sum share it
-  if (__any(mx > m + kLazy)) {
+  mx = fmaf(fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])), c2, -TreeRange<T16>::kLift);
+  // raised only where some lane's maximum grows by more than 2^kSlack: numerator and sum share it
+  if (__any(mx > m + TreeRange<T16>::kSlack)) {
     const float mn = fmaxf(m, mx);
     const float alpha = __builtin_amdgcn_exp2f(m - mn);
     m = mn;
@@ -413,7 +425,7 @@ __device__ __forceinline__ void tree_stream(const TreeArgs& a, int shares, int l
         const T16* vbase = reinterpret_cast<const T16*>(Vc);
 #pragma unroll
         for (int qi = 0; qi < QW; ++qi)
-          tree_softmax<DB>(s[qi], !cached || there < KT, cached ? tail : drafted[qi], fk, c2, m[qi], l[qi], o[qi]);
+          tree_softmax<T16, DB>(s[qi], !cached || there < KT, cached ? tail : drafted[qi], fk, c2, m[qi], l[qi], o[qi]);
         if (!cached) {
           bool odd = false;
 #pragma unroll
@@ -678,7 +690,7 @@ void k_tree_block(TreeArgs a, int shares, int least, int slack, int RB) {
       read_k(R, kf);
       scores(kf, s);
       const uint32_t vis = tree_word(a, b, ri, d, nn);
-      tree_softmax<DB>(s, true, vis, fk, c2, m, l, o);
+      tree_softmax<T16, DB>(s, true, vis, fk, c2, m, l, o);
       u32x4_t* Vc = R + KT * CH;
       bool odd = false;  // (every wave looks at the whole tile, so that all of them agree)
 #pragma unroll 2
@@ -759,7 +771,7 @@ void k_tree_block(TreeArgs a, int shares, int least, int slack, int RB) {
           scores(kf, s);
           read_v(now, vf);
           const int there = n0 - (from + k) * KT;
-          tree_softmax<DB>(s, there < KT, (1u << (there & 31)) - 1, fk, c2, m, l, o);
+          tree_softmax<T16, DB>(s, there < KT, (1u << (there & 31)) - 1, fk, c2, m, l, o);
           values(vf, s);
         }
       };

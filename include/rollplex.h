@@ -415,7 +415,7 @@ rp_status rp_pages_compact(const rp_pages *pages, void *stream, int32_t *n_live,
  *   (dev int32), trees by parents (dev int32 [B*N], the index of a node's parent
  *   among its sequence's; outside [0, i) = none; NULL = chains i-1), node i at rotary position
  *   pos0[b] + its depth (pos0 dev int32 [B]; NULL = len[b], after M-RoPE prompts
- *   the next rotary position).  A node sees the cache, its ancestors and itself.
+ *   the next rotary position; the sum is clamped to [0, max_position-1]).  A node sees the cache, its ancestors and itself.
  *   draft receives the new tokens' K/V of every layer ([B*N] rows, layer_stride
  *   apart), logits (optional fp32 [B*N, V]) their logits and next_ids [B*N] the
  *   argmax (lowest id on ties); padding rows hold unspecified numbers.  The cache is read only.

@@ -811,9 +811,9 @@ void k_tree_block(TreeArgs a, int shares, int least, int slack, int RB) {
 // ------------------------------------------------------------------------------------
 // fp32 on the fp32 matrix cores (v_mfma_f32_32x32x2: exact products), blocks of 32 rows whose NW waves
 // take the tiles of 32 keys in turn, fragments straight from global memory as in the prefix's fp32
-// kernel, and join their sums in LDS.  6 trees of 7 tokens over up to 577 keys (64): 10.4 us, a chain of
+// kernel, and join their sums in LDS.  6 trees of 7 tokens over up to 577 keys (64): 10.0 us, a chain of
 // loads (lengths, page ids, K, V) and 64 products of 64 cycles; 16 trees of 20 tokens over 3000 to 4000 keys
-// (128): 74 us, 45 TFLOP/s.
+// (128): 73 us, 47 TFLOP/s.
 // ------------------------------------------------------------------------------------
 template <int D, int NW>
 __global__ __launch_bounds__(NW * 64) void k_tree_f32(TreeArgs a, int shares, int least, int slack, int RB) {

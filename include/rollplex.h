@@ -343,8 +343,8 @@ rp_status rp_decode_step_static(const rp_model *model, void *stream, int32_t B, 
  *   refs    int32 [n_pages]: table entries in use that hold the page, 0 = free
  * page_size is a power of two in [8, 1024], table_ld*page_size <= 2^31 - 2^14 and
  * n_pages*page_size < 2^31 (else RP_ERR_UNSUPPORTED).  An empty pool is len = 0 and
- * refs = 0.  A full page may be shared; the page that a
- * sequence writes next never is.  The calls enqueue kernels only (no allocation,
+ * refs = 0.  A full page may be shared; the page that a sequence writes next never
+ * is.  The calls enqueue kernels only (no allocation,
  * copy or synchronisation), so they can be captured in a HIP graph.  Calls that
  * change one pool are ordered by the caller (one stream, or events).  Lengths
  * outside [0, table_ld*page_size] are clamped and page ids outside [0, n_pages)
@@ -415,7 +415,8 @@ rp_status rp_pages_compact(const rp_pages *pages, void *stream, int32_t *n_live,
  *   (dev int32), trees by parents (dev int32 [B*N], the index of a node's parent
  *   among its sequence's; outside [0, i) = none; NULL = chains i-1), node i at rotary position
  *   pos0[b] + its depth (pos0 dev int32 [B]; NULL = len[b], after M-RoPE prompts
- *   the next rotary position; the sum is clamped to [0, max_position-1]).  A node sees the cache, its ancestors and itself.
+ *   the next rotary position; the sum is clamped to [0, max_position-1]).  A node
+ *   sees the cache, its ancestors and itself.
  *   draft receives the new tokens' K/V of every layer ([B*N] rows, layer_stride
  *   apart), logits (optional fp32 [B*N, V]) their logits and next_ids [B*N] the
  *   argmax (lowest id on ties); padding rows hold unspecified numbers.  The cache is read only.

@@ -1326,21 +1326,25 @@ rp_status check_tree(const rp_pages& p, int32_t B, int32_t N) {
   return RP_OK;
 }
 
+// The attention's merge has a workgroup of 256 threads each 32 rows of a kv head; a launch of 2^32 threads runs as one of none.
+rp_status check_merge(int32_t B, int32_t N, int32_t Hq, int32_t Hkv) {
+  const int64_t merge = (int64_t)B * Hkv * (((int64_t)N * (Hq / Hkv) + 31) / 32);
+  if (merge >= 1 << 24)
+    return fail(RP_ERR_UNSUPPORTED, "batch %d * kv heads %d * rows of one / 32 = %lld, must be below 2^24", B, Hkv, (long long)merge);
+  return RP_OK;
+}
+
 rp_status check_tree_heads(const rp_pages& p, int32_t B, int32_t N, int32_t Hq) {
   if (p.head_dim != 64 && p.head_dim != 128) return fail(RP_ERR_UNSUPPORTED, "head_dim %d (supported: 64, 128)", p.head_dim);
   if (Hq < 1 || Hq % p.n_kv_heads) return fail(RP_ERR_SHAPE, "n_q_heads %d not a multiple of n_kv_heads %d", Hq, p.n_kv_heads);
   if (Hq / p.n_kv_heads > 8) return fail(RP_ERR_UNSUPPORTED, "query group size %d > 8", Hq / p.n_kv_heads);
-  // the merge has a workgroup of 256 threads each 32 rows of a kv head; a launch of 2^32 threads runs as one of none
-  const int64_t merge = (int64_t)B * p.n_kv_heads * (((int64_t)N * (Hq / p.n_kv_heads) + 31) / 32);
-  if (merge >= 1 << 24)
-    return fail(RP_ERR_UNSUPPORTED, "batch %d * kv heads %d * rows of one / 32 = %lld, must be below 2^24", B, p.n_kv_heads, (long long)merge);
-  return RP_OK;
+  return check_merge(B, N, Hq, p.n_kv_heads);
 }
 
 // A step's row kernels have a workgroup of up to 1024 threads a token.
-rp_status check_step_rows(int32_t B, int32_t N) {
+rp_status check_step_rows(const rp_config& c, int32_t B, int32_t N) {
   if ((int64_t)B * N >= 1 << 22) return fail(RP_ERR_UNSUPPORTED, "a step of %lld new tokens, must be below 2^22", (long long)B * N);
-  return RP_OK;
+  return check_merge(B, N, c.n_q_heads, c.n_kv_heads);
 }
 
 rp::TreeArgs tree_args(const rp_pages& p, int32_t B, int32_t N, int32_t Hq, const int32_t* n_nodes, const uint32_t* mask) {
@@ -1528,7 +1532,7 @@ rp_status rp_tree_step_workspace_bytes(const rp_model* m, int32_t B, int32_t N, 
   if (!m || !bytes) return fail(RP_ERR_INVALID_ARG, "model and bytes are required");
   if (B < 1 || N < 1 || N > RP_MAX_NODES) return fail(RP_ERR_SHAPE, "batch %d, new tokens %d outside [1, %d]", B, N, RP_MAX_NODES);
   if ((int64_t)B * N > 1 << 24) return fail(RP_ERR_UNSUPPORTED, "batch * new tokens exceeds 2^24");
-  const rp_status st = check_step_rows(B, N);
+  const rp_status st = check_step_rows(m->cfg, B, N);
   if (st != RP_OK) return st;
   *bytes = tree_ws(m, B, N, nullptr, nullptr);
   return RP_OK;
@@ -1539,13 +1543,12 @@ rp_status rp_tree_step(const rp_model* m, void* stream, const rp_pages* pages, i
                        int32_t* next_ids, void* ws, size_t ws_bytes) {
   if (!m) return fail(RP_ERR_INVALID_ARG, "model is NULL");
   rp_status st = check_pages(pages);
-  if (st != RP_OK || (st = check_tree(*pages, B, N)) != RP_OK || (st = check_step_rows(B, N)) != RP_OK) return st;
+  if (st != RP_OK || (st = check_tree(*pages, B, N)) != RP_OK || (st = check_step_rows(m->cfg, B, N)) != RP_OK) return st;
   const rp_config& c = m->cfg;
   if (pages->dtype != c.dtype || pages->n_layers != c.n_layers || pages->n_kv_heads != c.n_kv_heads || pages->head_dim != c.head_dim)
     return fail(RP_ERR_SHAPE, "pages: type, layers and heads must be the model's");
   if (c.dtype == RP_BF16 && c.head_dim == 64)
     return fail(RP_ERR_UNSUPPORTED, "rp_tree_step is disabled for bf16 models at head_dim 64, as rp_decode_step is");
-  if ((st = check_tree_heads(*pages, B, N, c.n_q_heads)) != RP_OK) return st;
   const int64_t R = (int64_t)B * N;
   if ((st = check_rows(*pages, draft, R, "draft")) != RP_OK) return st;
   if (!token_ids || !next_ids) return fail(RP_ERR_INVALID_ARG, "token_ids and next_ids are required");

@@ -45,3 +45,17 @@ def test_steps_of_more_tokens_than_a_launch_has_rows_for():
         refused(rb.RP_ERR_UNSUPPORTED, "2\\^22", rb.rp_tree_step, h, 0, p, 1 << 16, 64, None, FAKE, None, None, draft, None, FAKE, FAKE, 1 << 60)
     finally:
         rb.rp_destroy(h)
+
+
+def test_a_steps_merge_is_bounded_where_its_workspace_is_asked_for():
+    import dataclasses
+
+    m = dataclasses.replace(configs.TINY, n_q_heads=64, n_kv_heads=64, head_dim=64)
+    w, keep = fake_weights(m)
+    h = rb.rp_create(rb.make_config(m, 1024), w)
+    try:
+        assert rb.rp_tree_step_workspace_bytes(h, (1 << 18) - 1, 1) > 0
+        refused(rb.RP_ERR_UNSUPPORTED, "kv heads", rb.rp_tree_step_workspace_bytes, h, 1 << 18, 1)
+        refused(rb.RP_ERR_UNSUPPORTED, "kv heads", rb.rp_tree_step_workspace_bytes, h, 1 << 18, 8)
+    finally:
+        rb.rp_destroy(h)
